@@ -464,6 +464,133 @@ tod_status tod_loci(const float* x, int64_t n, int64_t d, const double* radii, i
                     int32_t* n_r_out, double* mdef_out, double* sigma_mdef_out,
                     tod_stats* stats);
 
+/*
+ * Sequence operators: rows for the detectors from token sequences.
+ *
+ * The rows that outlier detectors score are often a language model's hidden
+ * states.  These operators are what such a model needs beside its matrix
+ * products: attention over packed prompts, and a paged cache of keys and
+ * values with attention of each sequence's newest tokens over it.
+ *
+ * They differ from the calls above in three ways: tensors are fp16 or bf16
+ * (TOD_PREC_FP16, TOD_PREC_BF16); lengths, tables and slots are read on the
+ * device; and a call returns once its work is queued on `stream`, without
+ * waiting and without allocating, so that it may be captured into a HIP graph.
+ * The status therefore covers the arguments and the launch, not the values
+ * that lengths and tables hold: those never lead outside the buffers whose
+ * sizes are given, whatever they are, and each operator says what becomes of
+ * values out of range.  All buffers stay untouched by others until the work is
+ * done.  tod_last_error() works as for the calls above.
+ *
+ * Packed sequences: n_seq sequences share `tokens` rows; sequence s holds the
+ * rows row_start[s] .. row_start[s + 1] - 1 (int32 [n_seq + 1], ascending from
+ * 0; entries are cut to [0, tokens]).  Sequences may be empty.
+ *
+ * Paged cache: k_pages and v_pages are [n_pages, kv_heads, page_rows, dim],
+ * contiguous.  table[n_seq, table_cols] (int32) holds a sequence's pages in
+ * order: the token at position p lies in page table[s][p / page_rows], row
+ * p % page_rows; its slot is page * page_rows + row.
+ */
+
+/*
+ * Map of the cache for a step: pages and slots of every sequence's new tokens.
+ * cached[s] tokens of sequence s lie in the cache and fresh[s] follow (int32;
+ * negative counts as 0).  With P = page_rows and C = table_cols,
+ *   have(s) = min(ceil(cached / P), C)
+ *   need(s) = min(ceil((cached + fresh) / P), C) - have(s)
+ * The pages needed, over the sequences in order, take free_pages[0 .. n_free)
+ * from its start, -1 where it ends; table[s][have .. have + need) receives
+ * them, other entries stay.  The call may be repeated on its own result.
+ *   row_start_out[n_seq + 1] int32: packed rows of the new tokens
+ *   slot_out[tokens] int64: the slot of every new token; -1 where it has no
+ *                    page, its position lies past the table, or the row past
+ *                    the last sequence
+ *   pos_out[tokens]  int32, nullable: its position (cached + its number), or
+ *                    -1 for rows past the last sequence
+ *   used_out[2]      int64, nullable: pages needed, and new tokens left
+ *                    without a slot (free_pages at its end, the table at its
+ *                    last column or without the page that was begun, or more
+ *                    new tokens than `tokens`: those are left out and need no
+ *                    pages).  Entries of free_pages are page ids >= 0.
+ */
+tod_status tod_page_map(const int32_t* cached, const int32_t* fresh, int64_t n_seq,
+                        const int32_t* free_pages, int64_t n_free, int32_t page_rows,
+                        int32_t* table, int64_t table_cols, int64_t tokens, void* stream,
+                        int32_t* row_start_out, int64_t* slot_out, int32_t* pos_out,
+                        int64_t* used_out);
+
+/*
+ * Write of new keys and values into their slots (16-bit elements of any type,
+ * moved unchanged).  k, v: [tokens, kv_heads, dim], elements of a row
+ * contiguous; *_row and *_head are the strides of tokens and heads in elements,
+ * multiples of 8 (0: contiguous).  A token whose slot is outside
+ * [0, n_pages * page_rows) is left out; of tokens that share a slot, either
+ * may end up in it.  dim is a multiple of 8; tensors are 16-byte aligned.
+ */
+tod_status tod_page_write(const void* k, const void* v, int64_t tokens, int32_t kv_heads,
+                          int32_t dim, int64_t k_row, int64_t k_head, int64_t v_row,
+                          int64_t v_head, const int64_t* slot, void* k_pages, void* v_pages,
+                          int64_t n_pages, int32_t page_rows, void* stream);
+
+/* Heads, types and strides of an attention call. */
+typedef struct {
+  uint32_t struct_size; /* must be sizeof(tod_attn) */
+  int32_t precision;    /* of q, k, v and out: TOD_PREC_FP16 or TOD_PREC_BF16 */
+  int32_t heads;        /* query heads */
+  int32_t kv_heads;     /* key / value heads; query head h reads head h / (heads / kv_heads) */
+  int32_t dim;          /* elements of a head: a multiple of 8, at most 256 */
+  int32_t causal;       /* 1: a token sees itself and those before it; 0 (tod_attn_prompt only):
+                         * all of its sequence */
+  float scale;          /* of q k^T, finite, > 0; 0: 1 / sqrt(dim) */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+                        /* strides of tokens and heads in elements, multiples of 8; 0: those of a
+                         * contiguous [tokens, heads, dim].  The elements of a head are
+                         * contiguous.  k_* and v_*: tod_attn_prompt only. */
+} tod_attn;
+
+void tod_default_attn(tod_attn* attn, int32_t heads, int32_t kv_heads, int32_t dim,
+                      int32_t precision);
+
+/*
+ * Attention over whole packed prompts.  For query head h of token i, over the
+ * tokens j of the same sequence that i sees:
+ *   s_j = scale <q_i, k_j>,  out_i = sum_j exp(s_j) v_j / sum_j exp(s_j),
+ *   lse_i = ln sum_j exp(s_j)
+ * in one pass with fp32 products, maxima, sums and accumulators (the weights
+ * are rounded to the input type for their product with v).
+ *   q [tokens, heads, dim], k, v [tokens, kv_heads, dim]; 16-byte aligned
+ *   out [tokens, heads, dim] contiguous; lse_out [tokens, heads] fp32, nullable
+ * A row that sees no key, such as one past row_start[n_seq], gets 0 and -inf.
+ * Workspace: tod_attn_workspace_size(attn, tokens, n_seq, tokens) bytes, 256-byte
+ * aligned (0: invalid sizes); nothing in it lasts beyond the call.
+ */
+size_t tod_attn_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_seq,
+                               int64_t max_fresh);
+tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, const void* v,
+                           int64_t tokens, const int32_t* row_start, int64_t n_seq,
+                           void* workspace, size_t ws_bytes, void* stream, void* out,
+                           float* lse_out);
+
+/*
+ * Attention of every sequence's new tokens over its pages: chunks of a prompt,
+ * single tokens, or both.  Sequence s has cached[s] tokens in the cache before
+ * this step, and its rows of q are the tokens that follow, whose keys and
+ * values have been written too: token i of them sees the positions
+ * 0 .. cached[s] + i (at most table_cols * page_rows of them).  Formulas and outputs
+ * as tod_attn_prompt; attn->causal must be 1.  An entry of the table that is
+ * no page counts as a page of zeros.
+ *   max_fresh  no sequence has more new tokens than this (tokens is always
+ *              right).  Rows of a sequence that has are unspecified.
+ * Workspace: tod_attn_workspace_size(attn, tokens, n_seq, max_fresh) bytes,
+ * 256-byte aligned (0: invalid sizes); nothing in it lasts beyond the call.
+ */
+tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pages,
+                          const void* v_pages, int64_t n_pages, int32_t page_rows,
+                          const int32_t* table, int64_t table_cols, const int32_t* row_start,
+                          const int32_t* cached, int64_t n_seq, int64_t tokens,
+                          int64_t max_fresh, void* workspace, size_t ws_bytes, void* stream,
+                          void* out, float* lse_out);
+
 /* Static string naming a status code. */
 const char* tod_status_string(tod_status status);
 

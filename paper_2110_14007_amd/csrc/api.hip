@@ -16,6 +16,7 @@
 #include <string>
 #include <vector>
 
+#include "seq.h"
 #include "tod_internal.h"
 
 namespace {
@@ -108,6 +109,17 @@ tod_status check_sizes(int64_t nq, int64_t nr, int64_t d, int32_t k, int32_t exc
 }
 
 }  // namespace
+
+namespace tod {
+tod_status set_error(tod_status s, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {
+    g_last_error.clear();
+  }
+  return s;
+}
+}  // namespace tod
 
 namespace tod {
 

@@ -1,0 +1,73 @@
+// Device-side arguments of the sequence operators (page map, page write,
+// attention) and the launch functions of their kernels.  Not part of the
+// public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/tod.h"
+
+namespace tod {
+
+// Division of a 32-bit unsigned number below 2^31 by a constant d >= 1 that is
+// known at run time only: n / d = (n * mul) >> 32 >> shift with
+// mul = floor(2^(32 + shift) / d) + 1 and 2^shift <= d < 2^(shift + 1).  The
+// error term n / 2^(32 + shift) stays below 1 / d for n < 2^31 < 2^32.
+struct FastDiv {
+  uint32_t d, mul, shift;
+};
+
+inline FastDiv fast_div(uint32_t d) {
+  FastDiv f{d, 0, 0};
+  while ((2ull << f.shift) <= d) ++f.shift;
+  const uint64_t m = (1ull << (32 + f.shift)) / d + 1;
+  f.mul = m > 0xffffffffull ? 0 : (uint32_t)m;  // d = 2^shift: mul would be 2^32 + 1
+  return f;
+}
+
+__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
+  return (f.mul ? __umulhi(n, f.mul) : n) >> f.shift;
+}
+
+struct PageMapArgs {
+  const int32_t *cached, *fresh, *free_pages;
+  int64_t n_seq, n_free, cols, tokens;
+  FastDiv page;
+  int32_t *table, *row_start, *pos;
+  int64_t *slot, *used;
+};
+
+struct PageWriteArgs {
+  const void *k, *v;
+  int64_t k_row, k_head, v_row, v_head;  // strides in elements
+  const int64_t* slot;
+  void *k_pages, *v_pages;
+  int64_t tokens, slots;  // slots: n_pages * page
+  FastDiv page, per_token, per_row;  // 16-byte pieces of a token and of one head's row
+  int32_t kv_heads;
+};
+
+struct AttnArgs {
+  const void *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
+  const int32_t *row_start, *cached, *table;            // cached, table: paged only
+  int64_t cols;
+  int32_t n_seq, tokens, n_pages;
+  FastDiv page, group;  // rows of a page; query heads per key / value head
+  int32_t heads, kv_heads, dim;
+  int32_t causal;
+  float scale;  // of q k^T, times log2(e)
+  void* out;
+  float* lse;
+};
+
+hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
+hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
+hipError_t launch_attn_f16(const AttnArgs& a, bool paged, hipStream_t s);
+hipError_t launch_attn_bf16(const AttnArgs& a, bool paged, hipStream_t s);
+
+// Records a call's error for tod_last_error (never throws) and returns it.
+tod_status set_error(tod_status s, const char* msg) noexcept;
+
+}  // namespace tod

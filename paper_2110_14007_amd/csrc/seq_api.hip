@@ -1,0 +1,282 @@
+// Host side of the sequence operators: argument checks and launches.  Nothing
+// here waits for the GPU or allocates, so the calls may be captured into a
+// HIP graph.
+#include <math.h>
+#include <stdio.h>
+#include <string.h>
+
+#include "seq.h"
+
+namespace {
+
+using tod::set_error;
+
+constexpr int64_t kMaxCount = 0x7fffffffLL;
+
+tod_status invalid(const char* msg) { return set_error(TOD_ERR_INVALID_ARG, msg); }
+tod_status unsupported(const char* msg) { return set_error(TOD_ERR_UNSUPPORTED, msg); }
+
+tod_status launched(hipError_t e, const char* where) {
+  if (e == hipSuccess) return TOD_OK;
+  char msg[256];
+  snprintf(msg, sizeof(msg), "%s: %s", where, hipGetErrorString(e));
+  return set_error(TOD_ERR_HIP, msg);
+}
+
+bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+tod_status check_pages(int64_t n_pages, int32_t page_rows, int64_t kv_heads) {
+  if (page_rows <= 0 || page_rows > 65536)
+    return invalid("page_rows must be in [1, 65536]");
+  if (n_pages <= 0) return invalid("the cache needs at least one page");
+  if (n_pages > kMaxCount / page_rows / kv_heads)
+    return unsupported("more than 2^31 - 1 rows of all heads in the cache");
+  return TOD_OK;
+}
+
+// Sizes, types and strides that all attention calls share.  rows: the row and
+// head strides that *a leaves 0 become those of a contiguous [rows, heads, dim].
+tod_status check_attn(const tod_attn* a, tod_attn* out) {
+  if (!a) return invalid("null tod_attn");
+  if (a->struct_size != sizeof(tod_attn))
+    return invalid("tod_attn.struct_size does not match this library");
+  *out = *a;
+  if (a->precision != TOD_PREC_FP16 && a->precision != TOD_PREC_BF16)
+    return a->precision == TOD_PREC_FP32 || a->precision == TOD_PREC_AUTO
+               ? unsupported("attention takes fp16 or bf16 tensors")
+               : invalid("unknown precision");
+  if (a->heads <= 0 || a->kv_heads <= 0 || a->dim <= 0)
+    return invalid("heads, kv_heads and dim must be positive");
+  if (a->heads % a->kv_heads)
+    return invalid("heads must be a multiple of kv_heads");
+  if (a->dim % 8) return unsupported("dim must be a multiple of 8");
+  if (a->dim > 256) return unsupported("dim > 256");
+  if (a->heads > 65536) return unsupported("more than 65536 heads");
+  if (a->causal != 0 && a->causal != 1) return invalid("causal must be 0 or 1");
+  if (!(a->scale >= 0.0f) || isinf(a->scale))
+    return invalid("scale must be finite and positive (0: 1 / sqrt(dim))");
+  int64_t* const strides[6] = {&out->q_row, &out->q_head, &out->k_row,
+                               &out->k_head, &out->v_row, &out->v_head};
+  for (int i = 0; i < 6; ++i) {
+    if (*strides[i] < 0) return invalid("strides must not be negative");
+    if (*strides[i] % 8) return unsupported("strides must be multiples of 8 elements");
+    if (*strides[i] == 0)
+      *strides[i] = i % 2 ? a->dim : (int64_t)a->dim * (i == 0 ? a->heads : a->kv_heads);
+  }
+  if (out->scale == 0.0f) out->scale = 1.0f / sqrtf((float)a->dim);
+  return TOD_OK;
+}
+
+tod_status check_rows(const tod_attn& a, int64_t tokens, int64_t n_seq) {
+  if (tokens <= 0 || n_seq <= 0) return invalid("tokens and n_seq must be positive");
+  if (n_seq > kMaxCount / 2) return unsupported("more than 2^30 - 1 sequences");
+  const int64_t group = a.heads / a.kv_heads;
+  // Tile slots of a head: tokens * group / 128 + n_seq + 1; the grid is 32 bits.
+  if (tokens > kMaxCount / 2 / group || tokens * group / 128 + n_seq + 1 > kMaxCount / a.kv_heads)
+    return unsupported("too many rows for one call");
+  return TOD_OK;
+}
+
+void fill(const tod_attn& o, tod::AttnArgs* a) {
+  memset(a, 0, sizeof(*a));
+  a->q_row = o.q_row;
+  a->q_head = o.q_head;
+  a->k_row = o.k_row;
+  a->k_head = o.k_head;
+  a->v_row = o.v_row;
+  a->v_head = o.v_head;
+  a->heads = o.heads;
+  a->kv_heads = o.kv_heads;
+  a->dim = o.dim;
+  a->group = tod::fast_div((uint32_t)(o.heads / o.kv_heads));
+  a->page = tod::fast_div(1);
+  a->causal = o.causal;
+  a->scale = o.scale * 1.44269504088896341f;
+}
+
+tod_status check_workspace(const tod_attn* attn, int64_t tokens, int64_t n_seq, int64_t max_fresh,
+                           const void* workspace, size_t ws_bytes) {
+  if (!aligned(workspace, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
+  if (ws_bytes < tod_attn_workspace_size(attn, tokens, n_seq, max_fresh))
+    return set_error(TOD_ERR_WORKSPACE, "workspace smaller than tod_attn_workspace_size()");
+  return TOD_OK;
+}
+
+tod_status run_attn(const tod_attn& o, const tod::AttnArgs& a, bool paged, void* stream,
+                    const char* where) {
+  const hipStream_t s = (hipStream_t)stream;
+  return launched(o.precision == TOD_PREC_FP16 ? tod::launch_attn_f16(a, paged, s)
+                                               : tod::launch_attn_bf16(a, paged, s),
+                  where);
+}
+
+}  // namespace
+
+extern "C" {
+
+void tod_default_attn(tod_attn* a, int32_t heads, int32_t kv_heads, int32_t dim,
+                      int32_t precision) {
+  if (!a) return;
+  memset(a, 0, sizeof(*a));
+  a->struct_size = sizeof(*a);
+  a->precision = precision;
+  a->heads = heads;
+  a->kv_heads = kv_heads;
+  a->dim = dim;
+  a->causal = 1;
+}
+
+tod_status tod_page_map(const int32_t* cached, const int32_t* fresh, int64_t n_seq,
+                        const int32_t* free_pages, int64_t n_free, int32_t page_rows,
+                        int32_t* table, int64_t table_cols, int64_t tokens, void* stream,
+                        int32_t* row_start_out, int64_t* slot_out, int32_t* pos_out,
+                        int64_t* used_out) {
+  set_error(TOD_OK, "");
+  if (!cached || !fresh || !table || !row_start_out || !slot_out)
+    return invalid("null pointer");
+  if (n_seq <= 0 || tokens <= 0 || table_cols <= 0)
+    return invalid("n_seq, tokens and table_cols must be positive");
+  if (n_free < 0 || (n_free > 0 && !free_pages)) return invalid("free_pages missing");
+  if (page_rows <= 0 || page_rows > 65536) return invalid("page_rows must be in [1, 65536]");
+  if (n_seq > kMaxCount || tokens > kMaxCount || table_cols > kMaxCount / page_rows)
+    return unsupported("more than 2^31 - 1 sequences, tokens or positions");
+  if (!aligned(cached, 4) || !aligned(fresh, 4) || !aligned(free_pages, 4) ||
+      !aligned(table, 4) || !aligned(row_start_out, 4) || !aligned(pos_out, 4) ||
+      !aligned(slot_out, 8) || !aligned(used_out, 8))
+    return invalid("misaligned pointer");
+  tod::PageMapArgs a;
+  a.cached = cached;
+  a.fresh = fresh;
+  a.free_pages = free_pages;
+  a.n_seq = n_seq;
+  a.n_free = n_free;
+  a.cols = table_cols;
+  a.tokens = tokens;
+  a.page = tod::fast_div((uint32_t)page_rows);
+  a.table = table;
+  a.row_start = row_start_out;
+  a.pos = pos_out;
+  a.slot = slot_out;
+  a.used = used_out;
+  return launched(tod::launch_page_map(a, (hipStream_t)stream), "tod_page_map");
+}
+
+tod_status tod_page_write(const void* k, const void* v, int64_t tokens, int32_t kv_heads,
+                          int32_t dim, int64_t k_row, int64_t k_head, int64_t v_row,
+                          int64_t v_head, const int64_t* slot, void* k_pages, void* v_pages,
+                          int64_t n_pages, int32_t page_rows, void* stream) {
+  set_error(TOD_OK, "");
+  if (!k || !v || !slot || !k_pages || !v_pages) return invalid("null pointer");
+  if (tokens <= 0 || kv_heads <= 0 || dim <= 0)
+    return invalid("tokens, kv_heads and dim must be positive");
+  if (dim % 8) return unsupported("dim must be a multiple of 8");
+  if (k_row < 0 || k_head < 0 || v_row < 0 || v_head < 0)
+    return invalid("strides must not be negative");
+  if (k_row % 8 || k_head % 8 || v_row % 8 || v_head % 8)
+    return unsupported("strides must be multiples of 8 elements");
+  const tod_status st = check_pages(n_pages, page_rows, kv_heads);
+  if (st != TOD_OK) return st;
+  const int64_t per_row = dim / 8;
+  if (per_row > kMaxCount / kv_heads || tokens > (kMaxCount - 256) / (per_row * kv_heads))
+    return unsupported("more than 2^31 - 1 pieces of 16 bytes in one call");
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return invalid("tensors must be 16-byte aligned");
+  if (!aligned(slot, 8)) return invalid("misaligned pointer");
+  tod::PageWriteArgs a;
+  a.k = k;
+  a.v = v;
+  a.k_head = k_head ? k_head : dim;
+  a.v_head = v_head ? v_head : dim;
+  a.k_row = k_row ? k_row : (int64_t)kv_heads * dim;
+  a.v_row = v_row ? v_row : (int64_t)kv_heads * dim;
+  a.slot = slot;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.tokens = tokens;
+  a.slots = n_pages * page_rows;
+  a.page = tod::fast_div((uint32_t)page_rows);
+  a.per_token = tod::fast_div((uint32_t)(per_row * kv_heads));
+  a.per_row = tod::fast_div((uint32_t)per_row);
+  a.kv_heads = kv_heads;
+  return launched(tod::launch_page_write(a, (hipStream_t)stream), "tod_page_write");
+}
+
+size_t tod_attn_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_seq,
+                               int64_t max_fresh) {
+  tod_attn o;
+  if (check_attn(attn, &o) != TOD_OK || check_rows(o, tokens, n_seq) != TOD_OK || max_fresh <= 0)
+    return 0;
+  return 256;
+}
+
+tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, const void* v,
+                           int64_t tokens, const int32_t* row_start, int64_t n_seq,
+                           void* workspace, size_t ws_bytes, void* stream, void* out,
+                           float* lse_out) {
+  set_error(TOD_OK, "");
+  tod_attn o;
+  tod_status st = check_attn(attn, &o);
+  if (st != TOD_OK) return st;
+  if (!q || !k || !v || !row_start || !out || !workspace) return invalid("null pointer");
+  if ((st = check_rows(o, tokens, n_seq)) != TOD_OK) return st;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
+    return invalid("tensors must be 16-byte aligned");
+  if (!aligned(row_start, 4) || !aligned(lse_out, 4)) return invalid("misaligned pointer");
+  if ((st = check_workspace(attn, tokens, n_seq, tokens, workspace, ws_bytes)) != TOD_OK) return st;
+  tod::AttnArgs a;
+  fill(o, &a);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.row_start = row_start;
+  a.n_seq = (int32_t)n_seq;
+  a.tokens = (int32_t)tokens;
+  a.out = out;
+  a.lse = lse_out;
+  return run_attn(o, a, false, stream, "tod_attn_prompt");
+}
+
+tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pages,
+                          const void* v_pages, int64_t n_pages, int32_t page_rows,
+                          const int32_t* table, int64_t table_cols, const int32_t* row_start,
+                          const int32_t* cached, int64_t n_seq, int64_t tokens,
+                          int64_t max_fresh, void* workspace, size_t ws_bytes, void* stream,
+                          void* out, float* lse_out) {
+  set_error(TOD_OK, "");
+  tod_attn o;
+  tod_status st = check_attn(attn, &o);
+  if (st != TOD_OK) return st;
+  if (!q || !k_pages || !v_pages || !table || !row_start || !cached || !out || !workspace)
+    return invalid("null pointer");
+  if (!o.causal) return unsupported("attention over pages is causal");
+  if ((st = check_rows(o, tokens, n_seq)) != TOD_OK) return st;
+  if ((st = check_pages(n_pages, page_rows, o.kv_heads)) != TOD_OK) return st;
+  if (table_cols <= 0 || max_fresh <= 0)
+    return invalid("table_cols and max_fresh must be positive");
+  if (table_cols > (kMaxCount - tokens) / page_rows)
+    return unsupported("more than 2^31 - 1 positions");
+  if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+    return invalid("tensors must be 16-byte aligned");
+  if (!aligned(table, 4) || !aligned(row_start, 4) || !aligned(cached, 4) || !aligned(lse_out, 4))
+    return invalid("misaligned pointer");
+  if ((st = check_workspace(attn, tokens, n_seq, max_fresh, workspace, ws_bytes)) != TOD_OK)
+    return st;
+  tod::AttnArgs a;
+  fill(o, &a);
+  a.q = q;
+  a.k = k_pages;
+  a.v = v_pages;
+  a.row_start = row_start;
+  a.cached = cached;
+  a.table = table;
+  a.cols = table_cols;
+  a.n_pages = (int32_t)n_pages;
+  a.page = tod::fast_div((uint32_t)page_rows);
+  a.n_seq = (int32_t)n_seq;
+  a.tokens = (int32_t)tokens;
+  a.out = out;
+  a.lse = lse_out;
+  return run_attn(o, a, true, stream, "tod_attn_paged");
+}
+
+}  // extern "C"

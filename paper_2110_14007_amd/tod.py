@@ -32,7 +32,8 @@ SYMBOLS = ("tod_default_options", "tod_workspace_size", "tod_knn", "tod_knn_noal
            "tod_knn_score", "tod_lof", "tod_lof_ties_workspace_size", "tod_lof_ties",
            "tod_knn_decision", "tod_knn_classify", "tod_abod", "tod_cof", "tod_nwr_workspace_size",
            "tod_nwr", "tod_loci_workspace_size", "tod_loci",
-           "tod_plan", "tod_plan_workspace",
+           "tod_plan", "tod_plan_workspace", "tod_page_map", "tod_page_write",
+           "tod_default_attn", "tod_attn_workspace_size", "tod_attn_prompt", "tod_attn_paged",
            "tod_status_string", "tod_last_error")
 
 
@@ -86,6 +87,24 @@ class tod_stats(ctypes.Structure):
         out = {name: getattr(self, name) for name, _ in self._fields_ if name != "struct_size"}
         out["precision"] = PRECISION_NAMES.get(self.precision, self.precision)
         return out
+
+
+class tod_attn(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("precision", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("q_row", ctypes.c_int64),
+        ("q_head", ctypes.c_int64),
+        ("k_row", ctypes.c_int64),
+        ("k_head", ctypes.c_int64),
+        ("v_row", ctypes.c_int64),
+        ("v_head", ctypes.c_int64),
+    ]
 
 
 class TodError(RuntimeError):
@@ -143,6 +162,21 @@ def _load():
     lib.tod_plan.restype = ctypes.c_int
     lib.tod_plan_workspace.argtypes = [i64, i64, i64, i32, i32, opt_p, sz, st_p]
     lib.tod_plan_workspace.restype = ctypes.c_int
+    at_p = ctypes.POINTER(tod_attn)
+    lib.tod_page_map.argtypes = [vp, vp, i64, vp, i64, i32, vp, i64, i64, vp, vp, vp, vp, vp]
+    lib.tod_page_map.restype = ctypes.c_int
+    lib.tod_page_write.argtypes = [vp, vp, i64, i32, i32, i64, i64, i64, i64, vp, vp, vp, i64, i32,
+                                   vp]
+    lib.tod_page_write.restype = ctypes.c_int
+    lib.tod_default_attn.argtypes = [at_p, i32, i32, i32, i32]
+    lib.tod_default_attn.restype = None
+    lib.tod_attn_workspace_size.argtypes = [at_p, i64, i64, i64]
+    lib.tod_attn_workspace_size.restype = sz
+    lib.tod_attn_prompt.argtypes = [at_p, vp, vp, vp, i64, vp, i64, vp, sz, vp, vp, vp]
+    lib.tod_attn_prompt.restype = ctypes.c_int
+    lib.tod_attn_paged.argtypes = [at_p, vp, vp, vp, i64, i32, vp, i64, vp, vp, i64, i64, i64, vp,
+                                   sz, vp, vp, vp]
+    lib.tod_attn_paged.restype = ctypes.c_int
     lib.tod_status_string.argtypes = [ctypes.c_int]
     lib.tod_status_string.restype = ctypes.c_char_p
     lib.tod_last_error.argtypes = []
@@ -615,6 +649,234 @@ def tod_loci(x, radii, alpha: float = 0.5, n_min: int = 20, k_sigma: float = 3.0
     _check(rc, "tod_loci")
     del wsbuf
     return (score, flag, extra) if return_all else (score, flag)
+
+
+# ---------------------------------------------------------------------------
+# sequence operators: queued on the stream, not waited for
+# ---------------------------------------------------------------------------
+
+def _dev_tensor(x, name, dtypes, dim, device=None):
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
+    if x.dtype not in dtypes:
+        raise TypeError("%s must have dtype %s" % (name, " or ".join(str(d) for d in dtypes)))
+    if x.dim() != dim:
+        raise TypeError("%s must have %d dimensions" % (name, dim))
+    if device is not None and x.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
+    return x
+
+
+def _dev_array(x, name, dtype, dim, device=None):
+    _dev_tensor(x, name, (dtype,), dim, device)
+    if not x.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    return x
+
+
+def _strides(x, name):
+    """(token stride, head stride) of a [tokens, heads, dim] tensor for the library."""
+    tokens, heads, dim = x.shape
+    row, head, one = x.stride()
+    if one != 1 and dim > 1:
+        raise TypeError("the elements of a head of %s must be contiguous" % name)
+    if (row == 0 and tokens > 1) or (head == 0 and heads > 1):
+        raise ValueError("%s is broadcast over tokens or heads" % name)
+    return (row if tokens > 1 else 0), (head if heads > 1 else dim)
+
+
+class _On:
+    """The stream of a call.  Its work outlives the call, and torch's allocator gives freed
+    memory to the stream that it was allocated on: with a stream of the caller's, every tensor
+    of the call is recorded as used there."""
+
+    def __init__(self, stream, device):
+        torch = _torch()
+        self.current = torch.cuda.current_stream(device)
+        self.stream = self.current if stream is None else stream
+        if self.stream.device != device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        self.device = device
+        self.ptr = ctypes.c_void_p(self.stream.cuda_stream)
+
+    def call(self, where, fn, *args):
+        torch = _torch()
+        if torch.cuda.current_device() == self.device.index:
+            _check(fn(*args), where)
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*args), where)
+
+    def used(self, *tensors):
+        if self.stream.cuda_stream != self.current.cuda_stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+
+def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, stream=None):
+    """Pages and slots of every sequence's new tokens.
+
+    cached, fresh: int32 [n_seq]; free_pages: int32 [n_free]; table: int32 [n_seq, cols],
+    updated in place; tokens: the number of new tokens (a larger number pads the outputs).
+    -> (row_start int32 [n_seq + 1], slot int64 [tokens], pos int32 [tokens],
+        used int64 [2]: pages taken from free_pages, new tokens left without a slot)
+    """
+    torch = _torch()
+    _dev_array(cached, "cached", torch.int32, 1)
+    dev, n = cached.device, cached.shape[0]
+    _dev_array(fresh, "fresh", torch.int32, 1, dev)
+    _dev_array(free_pages, "free_pages", torch.int32, 1, dev)
+    _dev_array(table, "table", torch.int32, 2, dev)
+    if fresh.shape[0] != n or table.shape[0] != n:
+        raise ValueError("cached, fresh and table must have one row per sequence")
+    tokens = int(tokens)
+    on = _On(stream, dev)
+    room = max(tokens, 0)
+    out = torch.empty((2 + room,), dtype=torch.int64, device=dev)
+    rows = torch.empty((n + 1 + room,), dtype=torch.int32, device=dev)
+    used, slot, row_start, pos = out[:2], out[2:], rows[:n + 1], rows[n + 1:]
+    on.call("tod_page_map", _lib.tod_page_map, cached.data_ptr(), fresh.data_ptr(), n,
+            free_pages.data_ptr(), free_pages.shape[0], int(page_rows), table.data_ptr(),
+            table.shape[1], tokens, on.ptr, row_start.data_ptr(), slot.data_ptr(),
+            pos.data_ptr(), used.data_ptr())
+    on.used(cached, fresh, free_pages, table, out, rows)
+    return row_start, slot, pos, used
+
+
+def _pages(k_pages, v_pages, dtypes, device):
+    _dev_tensor(k_pages, "k_pages", dtypes, 4, device)
+    _dev_tensor(v_pages, "v_pages", (k_pages.dtype,), 4, device)
+    if k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages must have the same shape")
+    if not k_pages.is_contiguous() or not v_pages.is_contiguous():
+        raise TypeError("k_pages and v_pages must be contiguous")
+    return k_pages.shape
+
+
+def tod_page_write(k, v, slot, k_pages, v_pages, stream=None):
+    """Write k, v [tokens, kv_heads, dim] into their slots (int64 [tokens], negative: none) of
+    k_pages, v_pages [n_pages, kv_heads, page_rows, dim], in place."""
+    torch = _torch()
+    halves = (torch.float16, torch.bfloat16)
+    _dev_tensor(k, "k", halves, 3)
+    dev = k.device
+    _dev_tensor(v, "v", (k.dtype,), 3, dev)
+    _dev_array(slot, "slot", torch.int64, 1, dev)
+    n_pages, kv_heads, page_rows, dim = _pages(k_pages, v_pages, (k.dtype,), dev)
+    tokens = slot.shape[0]
+    if tuple(k.shape) != (tokens, kv_heads, dim) or v.shape != k.shape:
+        raise ValueError("k and v must be [%d, %d, %d] as slot and the pages are"
+                         % (tokens, kv_heads, dim))
+    on = _On(stream, dev)
+    (kr, kh), (vr, vh) = _strides(k, "k"), _strides(v, "v")
+    on.call("tod_page_write", _lib.tod_page_write, k.data_ptr(), v.data_ptr(), tokens, kv_heads,
+            dim, kr, kh, vr, vh, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
+            page_rows, on.ptr)
+    on.used(k, v, slot, k_pages, v_pages)
+
+
+def _attn(q, kv_heads, causal, scale):
+    torch = _torch()
+    a = tod_attn()
+    a.struct_size = ctypes.sizeof(tod_attn)
+    a.precision = PREC_FP16 if q.dtype == torch.float16 else PREC_BF16
+    a.heads, a.kv_heads, a.dim = q.shape[1], kv_heads, q.shape[2]
+    a.causal = int(bool(causal))
+    a.scale = 0.0 if scale is None else float(scale)
+    if scale is not None and not a.scale > 0.0:
+        raise ValueError("scale must be positive")
+    a.q_row, a.q_head = _strides(q, "q")
+    return a
+
+
+def _attn_outputs(q, out, return_lse):
+    torch = _torch()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device \
+            or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
+    return out, lse
+
+
+def tod_attn_workspace_size(heads: int, kv_heads: int, dim: int, tokens: int, n_seq: int,
+                            max_fresh=None) -> int:
+    """Workspace bytes of tod_attn_prompt and tod_attn_paged (0: sizes that they refuse)."""
+    a = tod_attn()
+    _lib.tod_default_attn(ctypes.byref(a), int(heads), int(kv_heads), int(dim), PREC_FP16)
+    return int(_lib.tod_attn_workspace_size(ctypes.byref(a), int(tokens), int(n_seq),
+                                            int(tokens if max_fresh is None else max_fresh)))
+
+
+def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspace=None,
+                    stream=None, out=None, return_lse: bool = False):
+    """Attention over whole packed prompts.
+
+    q [tokens, heads, dim], k, v [tokens, kv_heads, dim] (fp16 or bf16, any token and head
+    strides that are multiples of 8); row_start int32 [n_seq + 1].
+    -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
+    """
+    torch = _torch()
+    _dev_tensor(q, "q", (torch.float16, torch.bfloat16), 3)
+    dev = q.device
+    _dev_tensor(k, "k", (q.dtype,), 3, dev)
+    _dev_tensor(v, "v", (q.dtype,), 3, dev)
+    _dev_array(row_start, "row_start", torch.int32, 1, dev)
+    tokens, _, dim = q.shape
+    if k.shape != v.shape or k.shape[0] != tokens or k.shape[2] != dim:
+        raise ValueError("k and v must be [tokens, kv_heads, dim] with q's tokens and dim")
+    a = _attn(q, k.shape[1], causal, scale)
+    a.k_row, a.k_head = _strides(k, "k")
+    a.v_row, a.v_head = _strides(v, "v")
+    on = _On(stream, dev)
+    out, lse = _attn_outputs(q, out, return_lse)
+    n = row_start.shape[0] - 1
+    need = int(_lib.tod_attn_workspace_size(ctypes.byref(a), tokens, n, tokens))
+    wsbuf, wsp, wsn = _ws(workspace, need, dev)
+    on.call("tod_attn_prompt", _lib.tod_attn_prompt, ctypes.byref(a), q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), tokens, row_start.data_ptr(), n, wsp, wsn, on.ptr, out.data_ptr(),
+            lse.data_ptr() if return_lse else None)
+    on.used(q, k, v, row_start, out, lse, wsbuf)
+    return (out, lse) if return_lse else out
+
+
+def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None, scale=None,
+                   workspace=None, stream=None, out=None, return_lse: bool = False):
+    """Attention of every sequence's new tokens over its pages.
+
+    q [tokens, heads, dim]; k_pages, v_pages [n_pages, kv_heads, page_rows, dim], the new tokens'
+    keys and values written; table int32 [n_seq, cols]; row_start int32 [n_seq + 1]; cached int32
+    [n_seq]: tokens in the cache before this step.  max_fresh: the most new tokens of a sequence,
+    where the caller knows it.
+    -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
+    """
+    torch = _torch()
+    _dev_tensor(q, "q", (torch.float16, torch.bfloat16), 3)
+    dev = q.device
+    n_pages, kv_heads, page_rows, dim = _pages(k_pages, v_pages, (q.dtype,), dev)
+    _dev_array(table, "table", torch.int32, 2, dev)
+    _dev_array(row_start, "row_start", torch.int32, 1, dev)
+    _dev_array(cached, "cached", torch.int32, 1, dev)
+    tokens, n = q.shape[0], cached.shape[0]
+    if q.shape[2] != dim:
+        raise ValueError("q and the pages must have the same dim")
+    if table.shape[0] != n or row_start.shape[0] != n + 1:
+        raise ValueError("table, row_start and cached must describe the same sequences")
+    a = _attn(q, kv_heads, True, scale)
+    on = _On(stream, dev)
+    out, lse = _attn_outputs(q, out, return_lse)
+    fresh = tokens if max_fresh is None else int(max_fresh)
+    need = int(_lib.tod_attn_workspace_size(ctypes.byref(a), tokens, n, fresh))
+    wsbuf, wsp, wsn = _ws(workspace, need, dev)
+    on.call("tod_attn_paged", _lib.tod_attn_paged, ctypes.byref(a), q.data_ptr(),
+            k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_rows, table.data_ptr(),
+            table.shape[1], row_start.data_ptr(), cached.data_ptr(), n, tokens, fresh, wsp, wsn,
+            on.ptr, out.data_ptr(), lse.data_ptr() if return_lse else None)
+    on.used(q, k_pages, v_pages, table, row_start, cached, out, lse, wsbuf)
+    return (out, lse) if return_lse else out
 
 
 def raw_library():
