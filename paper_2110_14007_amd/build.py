@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libtod.so")
 SOURCES = ["api.hip", "prep.hip", "select.hip", "lof.hip", "tile_f32.hip", "tile_f16.hip",
            "tile_bf16.hip", "mtile_f16.hip", "mtile_bf16.hip", "order.hip",
            "rtile_f16.hip", "rtile_bf16.hip", "nwr.hip", "score.hip", "loci.hip",
-           "pages.hip", "seq_api.hip", "attn_f16.hip", "attn_bf16.hip"]
+           "pages.hip", "seq_api.hip", "attn_tile_f16.hip",
+           "attn_tile_bf16.hip", "attn_token_f16.hip", "attn_token_bf16.hip"]
 # The fused tile kernels take maxima of MFMA accumulators (fmax, so that the
 # compiler sees the reads and inserts the wait states an MFMA result needs
 # before a VALU reads it).  Their operands are never NaN (prep rejects
@@ -23,7 +24,8 @@ NO_NAN_SOURCES = {"mtile_f16.hip", "mtile_bf16.hip", "tile_f32.hip", "tile_f16.h
                   "tile_bf16.hip",
                   # (attention: scores may be NaN.  The maximum leaves them out, exp2 and the
                   # sums carry them to the output; nothing compares them with themselves.)
-                  "attn_f16.hip", "attn_bf16.hip"}
+                  "attn_tile_f16.hip", "attn_tile_bf16.hip", "attn_token_f16.hip",
+                  "attn_token_bf16.hip"}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

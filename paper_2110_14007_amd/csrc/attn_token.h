@@ -1,0 +1,291 @@
+// Attention of few new tokens a sequence over a paged cache (the single-token
+// form): bound by the bytes of the keys and values, each read once.
+//
+// The keys of all (sequence, key / value head) pairs, in stages of 32, form
+// one line that is dealt to the workers, a wave each, in equal shares, so that
+// neither one long sequence nor many of different lengths leave a part of the
+// GPU idle.  A wave works alone: it stages its keys and values in its own ring
+// of LDS buffers (the next stages are in flight while it computes), keeps up
+// to 32 packed rows and waits for nobody.  A pair that one wave reads whole is
+// finished by it; of the others each wave leaves (m, sum, O) and a second
+// kernel joins them.
+//
+// MFMAs and exponentials run far below the matrix rate (a stage of 16 KiB
+// takes one of 1280 waves about 4 us at the memory's rate, its arithmetic
+// 0.6), so p goes through the second product as two halves, the rounded p and
+// what the rounding lost: the output's rounding is then the only one.
+#pragma once
+
+#include "attn.h"
+
+namespace tod {
+namespace attn {
+
+constexpr int kTokenKeys = 32;  // keys of a stage
+constexpr int kTokenRows = kTokenMaxRows;
+
+// Buffers of a wave's ring, and loads of a stage.
+template <int DP>
+constexpr int token_ring() { return DP == 64 ? 4 : 2; }
+template <int DP>
+constexpr int token_loads() { return 2 * kTokenKeys * DP * 2 / 1024; }
+
+// Stages of a sequence that is the token kernel's, else 0.
+__device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
+  if (s >= a.n_seq) return 0;
+  const Seq q = seq_of<true>(a, s);
+  if (q.n <= 0 || (int64_t)q.n * a.group.d > a.skip_rows) return 0;
+  return (q.keys + kTokenKeys - 1) / kTokenKeys;
+}
+
+// Inclusive prefix sum over the lanes.
+__device__ __forceinline__ int64_t lane_prefix(int64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(v, d, 64);
+    if (lane >= d) v += y;
+  }
+  return v;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <typename ET, int DP>
+__global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
+  using V8 = typename Frag<ET>::V;
+  using St = Stager<ET, DP, true>;
+  constexpr int kStage = kTokenKeys * DP;  // elements of a K or V stage
+  constexpr int kRing = token_ring<DP>(), kLoads = token_loads<DP>(), DB = DP / 32;
+  __shared__ __align__(16) uint16_t lds[kRing * 2 * kStage];
+  const int lane = threadIdx.x, col = lane & 31, h = lane >> 5;
+
+  // Rows past the last sequence, where no tile kernel follows.
+  if (a.token_tail) {
+    const int32_t words = a.heads * a.dim / 8;
+    for (int32_t t = start_of(a, a.n_seq) + (int32_t)blockIdx.x; t < a.tokens;
+         t += (int32_t)gridDim.x) {
+      for (int32_t i = lane; i < words; i += 64)
+        ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
+      if (a.lse)
+        for (int32_t i = lane; i < a.heads; i += 64) a.lse[(int64_t)t * a.heads + i] = -INFINITY;
+    }
+  }
+
+  // The line of stages: lane l sums the sequences of its own segment.
+  const int32_t seg = (a.n_seq + 63) / 64, s0 = lane * seg;
+  int64_t mine = 0;
+  for (int32_t i = 0; i < seg; ++i) mine += token_stages(a, s0 + i);
+  const int64_t incl = lane_prefix(mine);
+  const int64_t total = __shfl(incl, 63, 64);  // of one head
+  const int64_t all = total * a.kv_heads;
+  const int64_t workers = min((int64_t)gridDim.x, all);
+  if (blockIdx.x == 0) {  // for the join
+    int64_t before = incl - mine;
+    for (int32_t i = 0; i < seg && s0 + i < a.n_seq; ++i) {
+      a.token_line[s0 + i] = before;
+      before += token_stages(a, s0 + i);
+    }
+    if (lane == 63) a.token_line[a.n_seq] = incl;
+  }
+  if ((int64_t)blockIdx.x >= workers) return;
+  int64_t at = all * (int64_t)blockIdx.x / workers;
+  const int64_t end = all * ((int64_t)blockIdx.x + 1) / workers;
+
+  // The sequence that holds stage `at`: its segment, then 64 sequences a step.
+  int32_t s;
+  int64_t off;  // of `at` in the sequence's stages of all heads
+  {
+    const int64_t target = at / a.kv_heads;
+    const int L = __popcll(__ballot(incl - mine <= target)) - 1;
+    int64_t before = __shfl(incl - mine, L, 64);
+    int32_t first = L * seg;
+    for (;;) {
+      const int32_t c = first + lane < (L + 1) * seg ? token_stages(a, first + lane) : 0;
+      const int64_t in = lane_prefix(c);
+      const int64_t sum = __shfl(in, 63, 64);
+      if (target < before + sum) {
+        const int k = __popcll(__ballot(before + in - c <= target)) - 1;
+        s = first + k;
+        before += __shfl(in - c, k, 64);
+        break;
+      }
+      before += sum;
+      first += 64;
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    off = at - before * a.kv_heads;
+  }
+
+  const uint32_t base = mt::lds_off(lds);
+  for (bool opening = true; at < end; opening = false) {
+    const Seq sq = seq_of<true>(a, s);
+    const int32_t stages = token_stages(a, s);
+    if (stages == 0) {  // another kernel's, or idle
+      ++s;
+      off = 0;
+      continue;
+    }
+    const uint32_t head = (uint32_t)(off / stages);
+    const int32_t jb = (int32_t)(off - (int64_t)head * stages);
+    const int32_t je = (int32_t)min((int64_t)stages, jb + (end - at));
+
+    const int32_t rows = sq.n * (int32_t)a.group.d;
+    const int32_t m = min(col, rows - 1);
+    const int32_t tok = (int32_t)div_by((uint32_t)m, a.group);
+    const int32_t qh = (int32_t)head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
+    const int32_t limit = min(sq.shift + tok, sq.keys - 1);
+    const int32_t wlo = __builtin_amdgcn_readfirstlane(limit);
+
+    St st(a, head);
+    st.seq = s;
+    st.start = sq.start;
+    st.seen = sq.keys;
+    auto stage = [&](int32_t j) {
+      const uint32_t pl = st.place(j * kTokenKeys, kTokenKeys);
+      const uint32_t k = base + 4u * kStage * (uint32_t)((j - jb) % kRing);
+#pragma unroll
+      for (int i = 0; i < kTokenKeys / St::kRowsLoad; ++i)
+        st.load(pl, i * St::kRowsLoad, k, k + 2u * kStage);
+    };
+#pragma unroll
+    for (int i = 0; i < kRing; ++i)
+      if (jb + i < je) stage(jb + i);
+
+    V8 q[DP / 16];
+    load_query<ET, DP>(
+        q, (const ET*)a.q + (int64_t)(sq.start + tok) * a.q_row + (int64_t)qh * a.q_head, a.dim, h);
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    float mref = kNoMax, sum = 0.0f;
+
+    for (int32_t j = jb; j < je; ++j) {
+      if (j + kRing <= je)
+        wait_loads<(kRing - 1) * kLoads>();
+      else
+        wait_loads<0>();
+      const uint16_t* const ks = lds + 2 * kStage * ((j - jb) % kRing);
+      const uint16_t* const vs = ks + kStage;
+      const int32_t j0 = j * kTokenKeys;
+      f32x16 x = scores<ET, DP>(ks, 0, q);
+      if (j0 + kTokenKeys - 1 > wlo) {
+        const int32_t left = limit - j0 - 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (mt::out_row_c(r) > left) x[r] = -INFINITY;
+      }
+      float top = x[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
+      top = fmaxf(top, other_half(top)) * a.scale;
+      const bool grow = top > mref;
+      if (__ballot(grow)) {
+        const float next = grow ? top : mref;
+        const float f = __builtin_amdgcn_exp2f(mref - next);
+        mref = next;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[d][r] *= f;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -mref));
+        sum += x[r];
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        typedef ET e8 __attribute__((ext_vector_type(8)));
+        e8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = x[8 * c + e];
+          hi[e] = (ET)p;
+          lo[e] = (ET)(p - (float)hi[e]);
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const V8 v = values<ET, DP>(vs, 16 * c, d);
+          o[d] = mfma<ET>(v, __builtin_bit_cast(V8, hi), o[d]);
+          o[d] = mfma<ET>(v, __builtin_bit_cast(V8, lo), o[d]);
+        }
+      }
+      if (j + kRing < je) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this buffer's reads are done
+        stage(j + kRing);
+      }
+    }
+    sum += other_half(sum);
+
+    if (col < rows) {
+      if (jb == 0 && je == stages) {
+        const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
+        store_row<ET, DP>(o, inverse(sum), (ET*)a.out + orow * a.dim, a.dim, h);
+        if (a.lse && h == 0) a.lse[orow] = log_sum(mref, sum);
+      } else {
+        // At most two of a worker's pieces are not whole: its first and its last.
+        const int64_t row = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows + col;
+        store_part<DP>(o, a.token_o + row * DP, h);
+        if (h == 0) a.token_stat[row] = {mref, sum};
+      }
+    }
+    // Its stores and LDS reads are done before the next pair's loads are counted.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    at += je - jb;
+    off += je - jb;
+    if (off == (int64_t)stages * a.kv_heads) {
+      ++s;
+      off = 0;
+    }
+  }
+}
+
+// Joins the pieces of a (sequence, key / value head) pair, one wave a row.
+template <typename ET, int DP>
+__global__ void __launch_bounds__(64) token_join_kernel(AttnArgs a, int64_t grid) {
+  uint32_t b = blockIdx.x;
+  const int32_t r = (int32_t)(b % (uint32_t)a.skip_rows);
+  b /= (uint32_t)a.skip_rows;
+  const uint32_t head = b % (uint32_t)a.kv_heads;
+  const int32_t s = (int32_t)(b / (uint32_t)a.kv_heads);
+  const int64_t before = a.token_line[s], stages = a.token_line[s + 1] - before;
+  if (stages == 0) return;
+  const int64_t all = a.token_line[a.n_seq] * a.kv_heads, workers = min(grid, all);
+  const int64_t lo = before * a.kv_heads + head * stages, hi = lo + stages;
+  // Worker w has the stages from floor(w all / workers) on.
+  const int64_t w0 = ((lo + 1) * workers - 1) / all, w1 = (hi * workers - 1) / all;
+  if (w0 == w1) return;
+  const Seq sq = seq_of<true>(a, s);
+  if (r >= sq.n * (int32_t)a.group.d) return;
+  const int32_t tok = (int32_t)div_by((uint32_t)r, a.group);
+  const int32_t qh = (int32_t)head * (int32_t)a.group.d + r - tok * (int32_t)a.group.d;
+  const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
+  // The first worker's piece is its last one if the pair begins within its share; the others
+  // begin with theirs.
+  const bool within = w0 * all / workers < lo;
+  const int64_t row0 = (2 * w0 + within) * a.skip_rows + r, row1 = 2 * (w0 + 1) * a.skip_rows + r;
+  join_row<ET, DP>(a.token_stat, a.token_o, row0, row1, 2 * (int64_t)a.skip_rows,
+                   (int32_t)(w1 - w0 + 1), (ET*)a.out + orow * a.dim,
+                   a.lse ? a.lse + orow : nullptr, a.dim);
+}
+
+template <typename ET, int DP>
+hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
+  const int64_t grid = token_workers(a.dim);
+  hipLaunchKernelGGL((token_kernel<ET, DP>), dim3((unsigned)grid), dim3(64), 0, s, a);
+  hipLaunchKernelGGL((token_join_kernel<ET, DP>),
+                     dim3((unsigned)((int64_t)a.n_seq * a.kv_heads * a.skip_rows)), dim3(64), 0, s,
+                     a, grid);
+  return hipGetLastError();
+}
+
+}  // namespace attn
+}  // namespace tod

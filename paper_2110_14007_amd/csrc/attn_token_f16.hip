@@ -1,0 +1,13 @@
+// Attention token kernel instantiations for fp16 inputs (see attn_token.h).
+#include "attn_token.h"
+
+namespace tod {
+
+hipError_t launch_attn_token_f16(const AttnArgs& a, hipStream_t s) {
+  using ET = _Float16;
+  if (a.dim <= 64) return attn::launch_token<ET, 64>(a, s);
+  if (a.dim <= 128) return attn::launch_token<ET, 128>(a, s);
+  return attn::launch_token<ET, 256>(a, s);
+}
+
+}  // namespace tod

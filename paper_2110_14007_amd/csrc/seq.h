@@ -60,12 +60,29 @@ struct AttnArgs {
   float scale;  // of q k^T, times log2(e)
   void* out;
   float* lse;
+  // Sequences of at most skip_rows packed rows are the token kernel's (0: none).
+  int32_t skip_rows, token_tail;
+  int64_t* token_line;  // [n_seq + 1]
+  float2* token_stat;   // [2 workers, skip_rows]
+  float* token_o;       // [2 workers, skip_rows, padded dim]
+  // Splits of a tile's keys.
+  int32_t tile_parts;
+  float2* tile_stat;  // [tiles of all heads, parts, 128]
+  float* tile_o;      // [tiles of all heads, parts, 128, padded dim]
 };
+
+// Packed rows that the token kernel takes: a product's 32 columns.
+constexpr int kTokenMaxRows = 32;
+// Its workers, as many waves as stay resident with their rings of LDS buffers (32 KiB, 64 KiB
+// for more than 128 elements) on 256 compute units of 160 KiB.
+inline int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1280; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
-hipError_t launch_attn_f16(const AttnArgs& a, bool paged, hipStream_t s);
-hipError_t launch_attn_bf16(const AttnArgs& a, bool paged, hipStream_t s);
+hipError_t launch_attn_tile_f16(const AttnArgs& a, bool paged, hipStream_t s);
+hipError_t launch_attn_tile_bf16(const AttnArgs& a, bool paged, hipStream_t s);
+hipError_t launch_attn_token_f16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_token_bf16(const AttnArgs& a, hipStream_t s);
 
 // Records a call's error for tod_last_error (never throws) and returns it.
 tod_status set_error(tod_status s, const char* msg) noexcept;

@@ -71,8 +71,10 @@ tod_status check_rows(const tod_attn& a, int64_t tokens, int64_t n_seq) {
   if (tokens <= 0 || n_seq <= 0) return invalid("tokens and n_seq must be positive");
   if (n_seq > kMaxCount / 2) return unsupported("more than 2^30 - 1 sequences");
   const int64_t group = a.heads / a.kv_heads;
-  // Tile slots of a head: tokens * group / 128 + n_seq + 1; the grid is 32 bits.
-  if (tokens > kMaxCount / 2 / group || tokens * group / 128 + n_seq + 1 > kMaxCount / a.kv_heads)
+  // Grids are 32 bits: a head's tile slots are tokens * group / 128 + n_seq + 1, with at most 16
+  // splits or 8 workgroups of the join each, and the tokens' join has 32 rows a sequence and head.
+  if (tokens > kMaxCount / 2 / group ||
+      tokens * group / 128 + n_seq + 1 > kMaxCount / 32 / a.kv_heads)
     return unsupported("too many rows for one call");
   return TOD_OK;
 }
@@ -94,20 +96,73 @@ void fill(const tod_attn& o, tod::AttnArgs* a) {
   a->scale = o.scale * 1.44269504088896341f;
 }
 
-tod_status check_workspace(const tod_attn* attn, int64_t tokens, int64_t n_seq, int64_t max_fresh,
-                           const void* workspace, size_t ws_bytes) {
-  if (!aligned(workspace, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
-  if (ws_bytes < tod_attn_workspace_size(attn, tokens, n_seq, max_fresh))
-    return set_error(TOD_ERR_WORKSPACE, "workspace smaller than tod_attn_workspace_size()");
-  return TOD_OK;
+// Workspace of a call, and how its work is split.
+struct Plan {
+  int32_t skip_rows, tile_parts;
+  bool tile;  // some sequence may have more rows than the token kernel takes
+  size_t line, token_stat, token_o, tile_stat, tile_o, total;
+};
+
+// paged: the call may hold sequences of few tokens for the token kernel.
+Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fresh, bool paged) {
+  Plan p;
+  memset(&p, 0, sizeof(p));
+  const int64_t group = o.heads / o.kv_heads;
+  const int64_t most = max_fresh < tokens ? max_fresh * group : tokens * group;
+  const int64_t dp = o.dim <= 64 ? 64 : o.dim <= 128 ? 128 : 256;
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += (size_t)((bytes + 255) / 256 * 256);
+    return here;
+  };
+  p.tile = !paged || most > tod::kTokenMaxRows;
+  if (paged && group <= tod::kTokenMaxRows) {
+    p.skip_rows = (int32_t)(most < tod::kTokenMaxRows ? most : tod::kTokenMaxRows / group * group);
+    const int64_t rows = 2 * tod::token_workers(o.dim) * p.skip_rows;
+    p.line = take((n_seq + 1) * 8);
+    p.token_stat = take(rows * 8);
+    p.token_o = take(rows * dp * 4);
+  }
+  p.tile_parts = 1;
+  if (p.tile) {
+    // Enough workgroups for four rounds of one on every compute unit, from the rows that there
+    // are; slots beside them stay empty.
+    const int64_t tiles = (tokens * group + 127) / 128 * o.kv_heads;
+    const int64_t slots = (tokens * group / 128 + n_seq + 1) * o.kv_heads;
+    const int64_t parts = 1024 / tiles;
+    p.tile_parts = (int32_t)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+    while (p.tile_parts > 1 && slots * p.tile_parts > 2048) --p.tile_parts;
+    if (p.tile_parts > 1) {
+      p.tile_stat = take(slots * p.tile_parts * 128 * 8);
+      p.tile_o = take(slots * p.tile_parts * 128 * dp * 4);
+    }
+  }
+  p.total = at ? at : 256;
+  return p;
 }
 
-tod_status run_attn(const tod_attn& o, const tod::AttnArgs& a, bool paged, void* stream,
-                    const char* where) {
+tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool paged, void* ws,
+                    size_t ws_bytes, void* stream, const char* where) {
+  if (!aligned(ws, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
+  if (ws_bytes < p.total)
+    return set_error(TOD_ERR_WORKSPACE, "workspace smaller than tod_attn_workspace_size()");
+  char* const base = (char*)ws;
+  a->skip_rows = p.skip_rows;
+  a->token_tail = p.tile ? 0 : 1;
+  a->token_line = (int64_t*)(base + p.line);
+  a->token_stat = (float2*)(base + p.token_stat);
+  a->token_o = (float*)(base + p.token_o);
+  a->tile_parts = p.tile_parts;
+  a->tile_stat = (float2*)(base + p.tile_stat);
+  a->tile_o = (float*)(base + p.tile_o);
   const hipStream_t s = (hipStream_t)stream;
-  return launched(o.precision == TOD_PREC_FP16 ? tod::launch_attn_f16(a, paged, s)
-                                               : tod::launch_attn_bf16(a, paged, s),
-                  where);
+  const bool half = o.precision == TOD_PREC_FP16;
+  hipError_t e = hipSuccess;
+  if (p.tile) e = half ? tod::launch_attn_tile_f16(*a, paged, s) : tod::launch_attn_tile_bf16(*a, paged, s);
+  if (e == hipSuccess && p.skip_rows)
+    e = half ? tod::launch_attn_token_f16(*a, s) : tod::launch_attn_token_bf16(*a, s);
+  return launched(e, where);
 }
 
 }  // namespace
@@ -206,7 +261,9 @@ size_t tod_attn_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_s
   tod_attn o;
   if (check_attn(attn, &o) != TOD_OK || check_rows(o, tokens, n_seq) != TOD_OK || max_fresh <= 0)
     return 0;
-  return 256;
+  const size_t paged = make_plan(o, tokens, n_seq, max_fresh, true).total;
+  const size_t prompt = make_plan(o, tokens, n_seq, max_fresh, false).total;
+  return paged > prompt ? paged : prompt;
 }
 
 tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, const void* v,
@@ -222,7 +279,6 @@ tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, c
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
     return invalid("tensors must be 16-byte aligned");
   if (!aligned(row_start, 4) || !aligned(lse_out, 4)) return invalid("misaligned pointer");
-  if ((st = check_workspace(attn, tokens, n_seq, tokens, workspace, ws_bytes)) != TOD_OK) return st;
   tod::AttnArgs a;
   fill(o, &a);
   a.q = q;
@@ -233,7 +289,8 @@ tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, c
   a.tokens = (int32_t)tokens;
   a.out = out;
   a.lse = lse_out;
-  return run_attn(o, a, false, stream, "tod_attn_prompt");
+  return run_attn(o, &a, make_plan(o, tokens, n_seq, tokens, false), false, workspace, ws_bytes,
+                  stream, "tod_attn_prompt");
 }
 
 tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pages,
@@ -259,8 +316,6 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
     return invalid("tensors must be 16-byte aligned");
   if (!aligned(table, 4) || !aligned(row_start, 4) || !aligned(cached, 4) || !aligned(lse_out, 4))
     return invalid("misaligned pointer");
-  if ((st = check_workspace(attn, tokens, n_seq, max_fresh, workspace, ws_bytes)) != TOD_OK)
-    return st;
   tod::AttnArgs a;
   fill(o, &a);
   a.q = q;
@@ -276,7 +331,8 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
   a.tokens = (int32_t)tokens;
   a.out = out;
   a.lse = lse_out;
-  return run_attn(o, a, true, stream, "tod_attn_paged");
+  return run_attn(o, &a, make_plan(o, tokens, n_seq, max_fresh, true), true, workspace, ws_bytes,
+                  stream, "tod_attn_paged");
 }
 
 }  // extern "C"
