@@ -144,6 +144,21 @@ struct Stager {
     }
   }
 
+  // Rows r0 .. r0 + kRowsLoad - 1 of a K (or V) stage that begins at LDS address `to`.
+  __device__ __forceinline__ void load_one(bool isk, uint32_t at, int r0, uint32_t to) const {
+    const int lane = threadIdx.x & 63;
+    const int r = r0 + lane / kPieces, pc = lane % kPieces;
+    const uint32_t row = (uint32_t)__shfl((int)at, r, 64);
+    const int c = 8 * (pc ^ (isk ? swizzle_k<DP>(r) : swizzle_v<DP>(r)));
+    const ET* p = (const ET*)(isk ? a.k : a.v);
+    if constexpr (PAGED)
+      p += (int64_t)row * a.dim;
+    else
+      p += (int64_t)row * (isk ? a.k_row : a.v_row) + (int64_t)head * (isk ? a.k_head : a.v_head);
+    const void* const src = row != ~0u && c < a.dim ? (const void*)(p + c) : &kZeros;
+    mt::dma16(src, to + 2u * (uint32_t)(r0 * DP));
+  }
+
   // Rows r0 .. r0 + kRowsLoad - 1 of a stage whose K begins at LDS address k and V at v; at: place().
   __device__ __forceinline__ void load(uint32_t at, int r0, uint32_t k, uint32_t v) const {
     const int lane = threadIdx.x & 63;

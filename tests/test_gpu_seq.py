@@ -352,3 +352,69 @@ def test_attn_paged_entries_that_are_no_page(env):
         q, kp, vp, torch.from_numpy(bad).cuda(), starts_of(torch, c["fresh"]),
         torch.tensor(c["cached"], dtype=torch.int32, device="cuda"), return_lse=True)
     check("bf16", out, lse, want, want_lse, float(vp.abs().max()))
+
+
+# ---------------------------------------------------------------------------
+# larger calls, against fp64 on the GPU
+# ---------------------------------------------------------------------------
+
+LARGE = {
+    "prompts_d128": dict(cached=[0] * 5, fresh=[4001, 1, 900, 0, 2333], hq=32, hk=8, d=128),
+    "prompts_d64": dict(cached=[0] * 3, fresh=[3000, 2999, 511], hq=24, hk=24, d=64),
+    "prompts_d96": dict(cached=[0] * 2, fresh=[5003, 640], hq=16, hk=16, d=96),
+    "prompts_d256": dict(cached=[0], fresh=[2100], hq=16, hk=4, d=256),
+    "prompts_one_head": dict(cached=[0], fresh=[9000], hq=1, hk=1, d=64),
+    "pages_d128": dict(cached=[3000, 10, 200], fresh=[1700, 1, 2900], hq=32, hk=8, d=128, page=16),
+    "pages_odd": dict(cached=[300, 777], fresh=[2000, 2500], hq=28, hk=4, d=80, page=12),
+    "pages_big": dict(cached=[1000], fresh=[4100], hq=32, hk=8, d=64, page=256),
+    "one_chunk": dict(cached=[20011], fresh=[130], hq=16, hk=2, d=128, page=32),
+    "tokens": dict(cached=[20000, 0, 511, 30001], fresh=[1, 3, 1, 2], hq=8, hk=2, d=128, page=16),
+}
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("name", sorted(LARGE))
+def test_attn_large(env, name, dt, causal):
+    torch, tod = env
+    c = LARGE[name]
+    paged = "page" in c
+    if paged and not causal:
+        pytest.skip("attention over pages is causal")
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    hq, hk, d, t = c["hq"], c["hk"], c["d"], sum(c["fresh"])
+    starts = starts_of(torch, c["fresh"])
+    if paged:
+        q, kp, vp, table = paged_case(torch, c, dt)
+        out, lse = tod.tod_attn_paged(
+            q, kp, vp, torch.from_numpy(table).cuda(), starts,
+            torch.tensor(c["cached"], dtype=torch.int32, device="cuda"),
+            max_fresh=max(c["fresh"]), return_lse=True)
+        v_max = float(vp.abs().max())
+    else:
+        qkv = rows(torch, gen, dt, t, hq + 2 * hk, d)
+        q, k, v = (1.5 * qkv[:, :hq]).to(qkv.dtype), qkv[:, hq:hq + hk], qkv[:, hq + hk:]
+        out, lse = tod.tod_attn_prompt(q, k, v, starts, causal=causal, return_lse=True)
+        v_max = float(v.abs().max())
+    bound, at = (2.5 * U[dt] + 2e-4) * v_max, 0
+    for r, (a, n) in enumerate(zip(c["cached"], c["fresh"])):
+        for h in range(0, hq, max(1, hq // 4)):
+            if paged:
+                j = np.arange(a + n)
+                pg = torch.from_numpy(table[r, j // c["page"]].astype(np.int64)).cuda()
+                row = torch.from_numpy(j % c["page"]).cuda()
+                kh, vh = (x[pg, h // (hq // hk), row].double() for x in (kp, vp))
+            else:
+                kh, vh = (x[at:at + n, h // (hq // hk)].double() for x in (k, v))
+            s = q[at:at + n, h].double() @ kh.T / math.sqrt(d)
+            if causal:
+                pos = torch.arange(a + n, device="cuda")
+                s = s.masked_fill(pos[None, :] > pos[a:a + n, None], -math.inf)
+            z = torch.logsumexp(s, dim=1)
+            want = torch.exp(s - z[:, None]) @ vh
+            if n:
+                err = float((out[at:at + n, h].double() - want).abs().max())
+                assert err <= bound, (r, h, err, bound)
+                off = float((lse[at:at + n, h].double() - z).abs().max())
+                assert off <= 1e-4, (r, h, off)
+        at += n
