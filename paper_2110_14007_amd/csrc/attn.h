@@ -108,11 +108,22 @@ __device__ __forceinline__ int swizzle_v(int row) {
   return DP == 64 ? 0 : (row & 3) << 1;
 }
 
+// mt::dma16 for data that no other wave reads: marked as streaming, so that it does not push
+// others' data out of the caches.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16_once(const void* g, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(g),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // Staging of keys and values for one wave, straight from global memory to LDS.
 // Over pages, lane l holds entry `first` + l of the sequence's table, so that
 // a stage (64 keys at most) finds its rows without a load from memory unless
 // it leaves those 64 pages.
-template <typename ET, int DP, bool PAGED>
+template <typename ET, int DP, bool PAGED, bool ONCE = false>
 struct Stager {
   static constexpr int kPieces = DP / 8;       // 16-byte pieces of a row
   static constexpr int kRowsLoad = 64 / kPieces;  // rows that one load of the wave moves
@@ -176,8 +187,13 @@ struct Stager {
     const bool ok = row != ~0u;
     const void* const ks = ok && ck < a.dim ? (const void*)(kp + ck) : &kZeros;
     const void* const vs = ok && cv < a.dim ? (const void*)(vp + cv) : &kZeros;
-    mt::dma16(ks, k + 2u * (uint32_t)(r0 * DP));
-    mt::dma16(vs, v + 2u * (uint32_t)(r0 * DP));
+    if constexpr (ONCE) {
+      dma16_once(ks, k + 2u * (uint32_t)(r0 * DP));
+      dma16_once(vs, v + 2u * (uint32_t)(r0 * DP));
+    } else {
+      mt::dma16(ks, k + 2u * (uint32_t)(r0 * DP));
+      mt::dma16(vs, v + 2u * (uint32_t)(r0 * DP));
+    }
   }
 };
 
@@ -273,20 +289,37 @@ __device__ __forceinline__ void join_row(const float2* stat, const float* o, int
   constexpr int C = DP / 64;
   const int lane = threadIdx.x & 63;
   auto row_of = [&](int32_t i) { return i == 0 ? row0 : row1 + (i - 1) * step; };
-  float m = kNoMax;
-  for (int32_t i = lane; i < parts; i += 64) m = fmaxf(m, stat[row_of(i)].x);
+  float m = kNoMax, sum = 0.0f, acc[C] = {};
+  for (int32_t i0 = 0; i0 < parts; i0 += 64) {  // 64 parts a turn, the statistics one a lane
+    const int32_t n = min(parts - i0, 64);
+    const float2 st = lane < n ? stat[row_of(i0 + lane)] : float2{kNoMax, 0.0f};
+    float top = fmaxf(m, st.x);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-  float sum = 0.0f, acc[C] = {};
-#pragma unroll 4
-  for (int32_t i = 0; i < parts; ++i) {
-    const int64_t row = row_of(i);
-    const float2 st = stat[row];
-    const float f = __builtin_amdgcn_exp2f(st.x - m);
-    sum += st.y * f;
-    const float* const p = o + row * DP + C * lane;
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(st.x - top);
+    m = top;
+    float part = st.y * f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] += p[c] * f;
+    for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d, 64);
+    sum = sum * keep + part;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] *= keep;
+    constexpr int kAhead = 8;  // parts in flight
+    for (int32_t i = 0; i < n; i += kAhead) {
+      float v[kAhead][C];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float* const p = o + row_of(i0 + min(i + k, n - 1)) * DP + C * lane;
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[k][c] = p[c];
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {  // a part past the last has weight 0 (i + k < 64)
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i + k));
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] += i + k < n ? v[k][c] * w : 0.0f;
+      }
+    }
   }
   const float inv = inverse(sum);
 #pragma unroll

@@ -17,7 +17,6 @@ constexpr int kRows = 32 * kWaves;  // rows of a workgroup
 constexpr int kWideWaves = 8, kWideRows = 32 * kWideWaves;  // of the wide kernel
 constexpr int kKeys = 64;           // keys of a stage
 constexpr float kSlack = 8.0f;  // growth of the maximum (log2) that m may lag behind
-constexpr int kMinStages = 8;   // of a split
 
 // What a workgroup works on.
 struct Tile : Seq {
@@ -57,7 +56,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int64_t b, Tile* t)
   const int32_t last = (int32_t)div_by((uint32_t)min(t->row0 + kRows - 1, t->rows - 1), a.group);
   t->seen = PAGED || a.causal ? min(t->shift + last + 1, t->keys) : t->keys;
   t->stages = (t->seen + kKeys - 1) / kKeys;
-  t->parts = max(min(a.tile_parts, t->stages / kMinStages), 1);
+  t->parts = max(min(a.tile_parts, t->stages / a.part_stages), 1);
   return true;
 }
 
@@ -184,8 +183,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
   sum += other_half(sum);
   if (t.row0 + 32 * wave + col >= t.rows) return;
   if (t.parts > 1) {
-    const int64_t row = (((slots - 1 - slot) * a.kv_heads + head) * a.tile_parts + part) * kRows +
-                        32 * wave + col;
+    const int64_t row = ((int64_t)b * a.tile_parts + part) * kRows + 32 * wave + col;
     store_part<DP>(o, a.tile_o + row * DP, h);
     if (h == 0) a.tile_stat[row] = {mref, sum};
     return;
@@ -230,12 +228,15 @@ __global__ void __launch_bounds__(64 * kWideWaves, 2) wide_kernel(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t b = blockIdx.x;
+  const uint32_t part = b % (uint32_t)a.tile_parts;
+  b /= (uint32_t)a.tile_parts;
   const uint32_t head = b % (uint32_t)a.kv_heads;
-  const int64_t slots = gridDim.x / (uint32_t)a.kv_heads;
+  const int64_t slots = gridDim.x / ((uint32_t)a.kv_heads * (uint32_t)a.tile_parts);
   const int64_t slot = slots - 1 - b / (uint32_t)a.kv_heads;
   Tile t;
-  if (!find_tile<PAGED, kRows>(a, slot, &t)) return;
-  const int32_t je = t.stages;
+  if (!find_tile<PAGED, kRows>(a, slot, &t) || (int)part >= t.parts) return;
+  const int32_t jb = (int32_t)((int64_t)t.stages * part / t.parts);
+  const int32_t count = (int32_t)((int64_t)t.stages * (part + 1) / t.parts) - jb;
 
   // This lane's query row, and the last key that it sees.
   const int32_t m = min(t.row0 + 32 * wave + col, t.rows - 1);
@@ -269,9 +270,10 @@ __global__ void __launch_bounds__(64 * kWideWaves, 2) wide_kernel(AttnArgs a) {
   // Whole stages whose rows of a wave lie together move by a base of the wave and an offset of
   // the lane that stays; the others (the last stage, small or odd pages, padded rows) one by one.
   const bool plain = a.dim == DP && (!PAGED || a.page.d % kRowsWave == 0);
-  auto stage = [&](bool isk, int32_t j) {
-    if (j >= je) return;
-    const uint32_t to = base + 2u * ((isk ? kbuf(j) : vbuf(j)) + (uint32_t)(wave * kRowsWave * DP));
+  auto stage = [&](bool isk, int32_t i0) {  // stage i0 of this split's
+    if (i0 >= count) return;
+    const int32_t j = jb + i0;
+    const uint32_t to = base + 2u * ((isk ? kbuf(i0) : vbuf(i0)) + (uint32_t)(wave * kRowsWave * DP));
     const int32_t j0 = j * kKeys + wave * kRowsWave;
     if (plain && (j + 1) * kKeys <= t.seen) {
       const ET* p;
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, 2) wide_kernel(AttnArgs a) {
     const uint32_t at = st.place(j * kKeys, kKeys);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      st.load_one(isk, at, wave * kRowsWave + i * St::kRowsLoad, base + 2u * (isk ? kbuf(j) : vbuf(j)));
+      st.load_one(isk, at, wave * kRowsWave + i * St::kRowsLoad, base + 2u * (isk ? kbuf(i0) : vbuf(i0)));
   };
 
   f32x16 o[DB];
@@ -426,18 +428,18 @@ __global__ void __launch_bounds__(64 * kWideWaves, 2) wide_kernel(AttnArgs a) {
     mt::dl_barrier<0>();
     stage(true, j + 2);
     stage(false, j + 1);
-    step(j * kKeys, std::integral_constant<int, r * kS + kH>{},
+    step((jb + j) * kKeys, std::integral_constant<int, r * kS + kH>{},
          std::integral_constant<int, (r + 2) % 3 * kS + kH>{});
-    step(j * kKeys + 32, std::integral_constant<int, (r + 1) % 3 * kS>{},
+    step((jb + j) * kKeys + 32, std::integral_constant<int, (r + 1) % 3 * kS>{},
          std::integral_constant<int, r * kS>{});
   };
-  for (int32_t j = 0; j < je; j += 3) {
+  for (int32_t j = 0; j < count; j += 3) {
     turn(j, std::integral_constant<int, 0>{});
-    if (j + 1 < je) turn(j + 1, std::integral_constant<int, 1>{});
-    if (j + 2 < je) turn(j + 2, std::integral_constant<int, 2>{});
+    if (j + 1 < count) turn(j + 1, std::integral_constant<int, 1>{});
+    if (j + 2 < count) turn(j + 2, std::integral_constant<int, 2>{});
   }
-  if (je > 0) {
-    const int at = (je - 1) % kRing * kS + kH;
+  if (count > 0) {
+    const int at = (count - 1) % kRing * kS + kH;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -446,27 +448,19 @@ __global__ void __launch_bounds__(64 * kWideWaves, 2) wide_kernel(AttnArgs a) {
   }
   sum += other_half(sum);
   if (t.row0 + 32 * wave + col >= t.rows) return;
+  if (t.parts > 1) {
+    const int64_t row = ((int64_t)b * a.tile_parts + part) * kRows + 32 * wave + col;
+    store_part<DP>(o, a.tile_o + row * DP, h);
+    if (h == 0) a.tile_stat[row] = {mref, sum};
+    return;
+  }
   const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
   store_row<ET, DP>(o, inverse(sum), (ET*)a.out + orow * a.dim, a.dim, h);
   if (a.lse && h == 0) a.lse[orow] = log_sum(mref, sum);
 }
 
-template <typename ET, int DP, bool PAGED>
-hipError_t launch_wide(const AttnArgs& a, hipStream_t s) {
-  const int64_t slots = (int64_t)a.tokens * a.group.d / kWideRows + a.n_seq + 1;
-  constexpr unsigned bytes = 2 * 3 * kKeys * DP * 2;  // three K and three V stages, 16 bits
-  const auto kern = wide_kernel<ET, DP, PAGED>;
-  if constexpr (bytes > 65536) {
-    const hipError_t e = hipFuncSetAttribute(
-        (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(kern, dim3((unsigned)(slots * a.kv_heads)), dim3(64 * kWideWaves), bytes, s, a);
-  return hipGetLastError();
-}
-
 // Joins the splits of a tile, one wave a row.
-template <typename ET, int DP, bool PAGED>
+template <typename ET, int DP, bool PAGED, int kRows>
 __global__ void __launch_bounds__(256) tile_join_kernel(AttnArgs a) {
   constexpr int kRowsGroup = 16;
   uint32_t b = blockIdx.x;
@@ -488,25 +482,35 @@ __global__ void __launch_bounds__(256) tile_join_kernel(AttnArgs a) {
   }
 }
 
-template <typename ET, int DP, bool PAGED>
-hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
-  if constexpr (DP <= 128)
-    if (a.tile_parts == 1 && (int64_t)a.tokens * a.group.d / kWideRows * a.kv_heads >= 512)
-      return launch_wide<ET, DP, PAGED>(a, s);
+template <typename ET, int DP, bool PAGED, int kRows>
+hipError_t launch_rows(const AttnArgs& a, hipStream_t s) {
+  constexpr bool wide = kRows == kWideRows;
   const int64_t slots = (int64_t)a.tokens * a.group.d / kRows + a.n_seq + 1;
-  constexpr unsigned bytes = 2 * 2 * kKeys * DP * 2;  // two buffers, K and V, 16 bits
-  const auto kern = tile_kernel<ET, DP, PAGED>;
+  constexpr unsigned bytes = 2 * (wide ? 3 : 2) * kKeys * DP * 2;  // K and V stages, 16 bits
+  constexpr unsigned threads = 64 * (wide ? kWideWaves : kWaves);
+  void (*kern)(AttnArgs);
+  if constexpr (wide)
+    kern = wide_kernel<ET, DP, PAGED>;
+  else
+    kern = tile_kernel<ET, DP, PAGED>;
   if constexpr (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)(slots * a.kv_heads * a.tile_parts)), dim3(64 * kWaves),
+  hipLaunchKernelGGL(kern, dim3((unsigned)(slots * a.kv_heads * a.tile_parts)), dim3(threads),
                      bytes, s, a);
   if (a.tile_parts > 1)
-    hipLaunchKernelGGL((tile_join_kernel<ET, DP, PAGED>),
+    hipLaunchKernelGGL((tile_join_kernel<ET, DP, PAGED, kRows>),
                        dim3((unsigned)(slots * a.kv_heads * (kRows / 16))), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+template <typename ET, int DP, bool PAGED>
+hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
+  if constexpr (DP <= 128)
+    if (a.tile_rows == kWideRows) return launch_rows<ET, DP, PAGED, kWideRows>(a, s);
+  return launch_rows<ET, DP, PAGED, kRows>(a, s);
 }
 
 }  // namespace attn

@@ -11,7 +11,7 @@
 // kernel joins them.
 //
 // MFMAs and exponentials run far below the matrix rate (a stage of 16 KiB
-// takes one of 1280 waves about 4 us at the memory's rate, its arithmetic
+// takes one of 1024 waves about 2.8 us at the memory's rate, its arithmetic
 // 0.6), so p goes through the second product as two halves, the rounded p and
 // what the rounding lost: the output's rounding is then the only one.
 #pragma once
@@ -57,7 +57,7 @@ __device__ __forceinline__ void wait_loads() {
 template <typename ET, int DP>
 __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   using V8 = typename Frag<ET>::V;
-  using St = Stager<ET, DP, true>;
+  using St = Stager<ET, DP, true, true>;
   constexpr int kStage = kTokenKeys * DP;  // elements of a K or V stage
   constexpr int kRing = token_ring<DP>(), kLoads = token_loads<DP>(), DB = DP / 32;
   __shared__ __align__(16) uint16_t lds[kRing * 2 * kStage];
@@ -103,7 +103,8 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
     const int L = __popcll(__ballot(incl - mine <= target)) - 1;
     int64_t before = __shfl(incl - mine, L, 64);
     int32_t first = L * seg;
-    for (;;) {
+    s = first;
+    while (seg > 1) {
       const int32_t c = first + lane < (L + 1) * seg ? token_stages(a, first + lane) : 0;
       const int64_t in = lane_prefix(c);
       const int64_t sum = __shfl(in, 63, 64);
@@ -250,21 +251,21 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
 
 // Joins the pieces of a (sequence, key / value head) pair, one wave a row.
 template <typename ET, int DP>
-__global__ void __launch_bounds__(64) token_join_kernel(AttnArgs a, int64_t grid) {
+__global__ void __launch_bounds__(64) token_join_kernel(AttnArgs a, int32_t grid) {
   uint32_t b = blockIdx.x;
   const int32_t r = (int32_t)(b % (uint32_t)a.skip_rows);
   b /= (uint32_t)a.skip_rows;
   const uint32_t head = b % (uint32_t)a.kv_heads;
   const int32_t s = (int32_t)(b / (uint32_t)a.kv_heads);
-  const int64_t before = a.token_line[s], stages = a.token_line[s + 1] - before;
-  if (stages == 0) return;
-  const int64_t all = a.token_line[a.n_seq] * a.kv_heads, workers = min(grid, all);
+  const int64_t before = a.token_line[s], after = a.token_line[s + 1];
+  const int64_t all = a.token_line[a.n_seq] * a.kv_heads, stages = after - before;
+  const Seq sq = seq_of<true>(a, s);
+  if (stages == 0 || r >= sq.n * (int32_t)a.group.d) return;
+  const int64_t workers = min((int64_t)grid, all);
   const int64_t lo = before * a.kv_heads + head * stages, hi = lo + stages;
   // Worker w has the stages from floor(w all / workers) on.
   const int64_t w0 = ((lo + 1) * workers - 1) / all, w1 = (hi * workers - 1) / all;
   if (w0 == w1) return;
-  const Seq sq = seq_of<true>(a, s);
-  if (r >= sq.n * (int32_t)a.group.d) return;
   const int32_t tok = (int32_t)div_by((uint32_t)r, a.group);
   const int32_t qh = (int32_t)head * (int32_t)a.group.d + r - tok * (int32_t)a.group.d;
   const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
@@ -283,7 +284,7 @@ hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((token_kernel<ET, DP>), dim3((unsigned)grid), dim3(64), 0, s, a);
   hipLaunchKernelGGL((token_join_kernel<ET, DP>),
                      dim3((unsigned)((int64_t)a.n_seq * a.kv_heads * a.skip_rows)), dim3(64), 0, s,
-                     a, grid);
+                     a, (int32_t)grid);
   return hipGetLastError();
 }
 

@@ -37,14 +37,20 @@ struct Pages {
   int64_t c, f, have, need;
 };
 
-__device__ __forceinline__ Pages pages_of(const PageMapArgs& a, int64_t r, int64_t start) {
+// ceil(n / P) for 0 <= n < 2^31.
+__device__ __forceinline__ int64_t pages_up(int64_t n, const FastDiv& page) {
+  return n == 0 ? 0 : (int64_t)div_by((uint32_t)n - 1u, page) + 1;
+}
+
+__device__ __forceinline__ Pages pages_of(const PageMapArgs& a, int32_t cached, int32_t fresh,
+                                          int64_t start) {
   Pages p;
-  p.c = max(a.cached[r], 0);
-  const int64_t room = max(a.tokens - start, (int64_t)0);
-  p.f = min((int64_t)max(a.fresh[r], 0), room);
-  const uint32_t up = a.page.d - 1;
-  p.have = min((int64_t)((p.c + up) / a.page.d), a.cols);
-  p.need = min((int64_t)((p.c + p.f + up) / a.page.d), a.cols) - p.have;
+  p.c = cached;
+  p.f = min((int64_t)fresh, max(a.tokens - start, (int64_t)0));
+  // Positions past the table need no more pages than it has columns; cols * P < 2^31.
+  const int64_t end = a.cols * a.page.d;
+  p.have = pages_up(min(p.c, end), a.page);
+  p.need = pages_up(min(p.c + p.f, end), a.page) - p.have;
   return p;
 }
 
@@ -67,48 +73,67 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   const bool first = blockIdx.x == 0;
   for (int i = tid; i < kMapTokens; i += kMapThreads) mark[i] = -1;
 
-  const int64_t per = (a.n_seq + kMapThreads - 1) / kMapThreads;
-  const int64_t r0 = min(tid * per, a.n_seq), r1 = min(r0 + per, a.n_seq);
-  int64_t fresh = 0;
-  for (int64_t r = r0; r < r1; ++r) fresh += max(a.fresh[r], 0);
-  int64_t all_fresh, all_need, lost_all;
-  const int64_t start0 = block_prefix(fresh, &all_fresh, sums);
-  int64_t need = 0, start = start0;
-  for (int64_t r = r0; r < r1; ++r) {
-    need += pages_of(a, r, start).need;
-    start += max(a.fresh[r], 0);
-  }
-  int64_t base = block_prefix(need, &all_need, sums);
-
-  int64_t lost = 0;
-  start = start0;
-  for (int64_t r = r0; r < r1; ++r) {
-    const Pages p = pages_of(a, r, start);
-    if (p.f > 0 && start < t1 && start + p.f > t0) {
-      const int at = (int)(max(start, t0) - t0);
-      mark[at] = at;
-      who[at] = (int32_t)r;
-      start_of[at] = start;
-      page_of[at] = base - p.have;  // free page of column c: page_of + c
+  // The sequences in rounds of kMapThreads * kEach, kEach neighbours a thread, with the sums so
+  // far in front.  Workgroups but the first leave when a round ends past their tokens.
+  constexpr int kEach = 8;
+  int64_t sum_fresh = 0, sum_need = 0, lost = 0;
+  for (int64_t q0 = 0; q0 < a.n_seq; q0 += kMapThreads * kEach) {
+    const int64_t r0 = q0 + tid * kEach;
+    int32_t c[kEach], f[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const bool in = r0 + i < a.n_seq;
+      c[i] = in ? max(a.cached[r0 + i], 0) : 0;
+      f[i] = in ? max(a.fresh[r0 + i], 0) : 0;
     }
-    if (first) {
-      a.row_start[r] = (int32_t)min(start, a.tokens);
-      // Tokens without a slot: cut off, past the pages, or in a page that the table lacks.
-      const int64_t got = p.have + min(max(a.n_free - base, (int64_t)0), p.need);
-      lost += max(a.fresh[r], 0) - p.f + max(p.c + p.f - max(p.c, got * a.page.d), (int64_t)0);
-      const int64_t open = p.c / a.page.d;  // column of the first new token
-      if (p.f > 0 && open < p.have && a.table[r * a.cols + open] < 0)
-        lost += min(p.f, p.have * a.page.d - p.c);
+    int64_t mine = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine += f[i];
+    int64_t start = sum_fresh + block_prefix(mine, &all, sums);
+    sum_fresh += all;
+    const int64_t start0 = start;
+    mine = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      mine += pages_of(a, c[i], f[i], start).need;
+      start += f[i];
     }
-    base += p.need;
-    start += max(a.fresh[r], 0);
+    int64_t base = sum_need + block_prefix(mine, &all, sums);
+    sum_need += all;
+    start = start0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int64_t r = r0 + i;
+      const Pages p = pages_of(a, c[i], f[i], start);
+      if (p.f > 0 && start < t1 && start + p.f > t0) {
+        const int at = (int)(max(start, t0) - t0);
+        mark[at] = at;
+        who[at] = (int32_t)r;
+        start_of[at] = start;
+        page_of[at] = base - p.have;  // free page of column c: page_of + c
+      }
+      if (first && r < a.n_seq) {
+        a.row_start[r] = (int32_t)min(start, a.tokens);
+        // Tokens without a slot: cut off, past the pages, or in a page that the table lacks.
+        const int64_t got = p.have + min(max(a.n_free - base, (int64_t)0), p.need);
+        lost += f[i] - p.f + max(p.c + p.f - max(p.c, got * a.page.d), (int64_t)0);
+        // The column of the first new token, if its page was begun before.
+        const int64_t open = p.have - 1;
+        if (p.f > 0 && p.c < p.have * a.page.d && a.table[r * a.cols + open] < 0)
+          lost += min(p.f, p.have * a.page.d - p.c);
+      }
+      base += p.need;
+      start += f[i];
+    }
+    if (!first && sum_fresh >= t1) break;
   }
   if (first) {
+    int64_t lost_all;
     block_prefix(lost, &lost_all, sums);
     if (tid == 0) {
-      a.row_start[a.n_seq] = (int32_t)min(all_fresh, a.tokens);
+      a.row_start[a.n_seq] = (int32_t)min(sum_fresh, a.tokens);
       if (a.used) {
-        a.used[0] = all_need;
+        a.used[0] = sum_need;
         a.used[1] = lost_all;
       }
     }
@@ -116,10 +141,10 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   __syncthreads();
 
   // Running maximum of the markers: four places a thread, then over the threads.
-  constexpr int kEach = kMapTokens / kMapThreads;
-  int m[kEach], top = -1;
+  constexpr int kPlaces = kMapTokens / kMapThreads;
+  int m[kPlaces], top = -1;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) m[i] = top = max(top, mark[tid * kEach + i]);
+  for (int i = 0; i < kPlaces; ++i) m[i] = top = max(top, mark[tid * kPlaces + i]);
   const int lane = tid & 63, wave = tid >> 6;
   int x = top;
 #pragma unroll
@@ -134,19 +159,19 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   __syncthreads();
   for (int w = 0; w < wave; ++w) prev = max(prev, (int)sums[w]);
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) mark[tid * kEach + i] = max(prev, m[i]);
+  for (int i = 0; i < kPlaces; ++i) mark[tid * kPlaces + i] = max(prev, m[i]);
   __syncthreads();
 
   for (int i = tid; i < (int)(t1 - t0); i += kMapThreads) {
     const int64_t t = t0 + i;
     const int at = mark[i];
     int64_t slot = -1, pos = -1;
-    if (at >= 0 && t < all_fresh) {
+    if (at >= 0 && t < sum_fresh) {
       const int64_t r = who[at];
       const int64_t c = max(a.cached[r], 0);
       pos = c + (t - start_of[at]);
-      const int64_t col = pos / a.page.d, in = pos - col * a.page.d;
-      if (col < a.cols) {
+      if (pos < a.cols * a.page.d) {
+        const int64_t col = div_by((uint32_t)pos, a.page), in = pos - col * a.page.d;
         int32_t* const entry = a.table + r * a.cols + col;
         int32_t page;
         if (col * a.page.d < c) {

@@ -66,16 +66,19 @@ struct AttnArgs {
   float2* token_stat;   // [2 workers, skip_rows]
   float* token_o;       // [2 workers, skip_rows, padded dim]
   // Splits of a tile's keys.
-  int32_t tile_parts;
-  float2* tile_stat;  // [tiles of all heads, parts, 128]
-  float* tile_o;      // [tiles of all heads, parts, 128, padded dim]
+  int32_t tile_rows;    // rows of a tile
+  int32_t tile_parts;   // most splits of one
+  int32_t part_stages;  // fewest stages (of 64 keys) of a split
+  float2* tile_stat;    // [tiles of all heads, parts, rows]
+  float* tile_o;        // [tiles of all heads, parts, rows, padded dim]
 };
 
 // Packed rows that the token kernel takes: a product's 32 columns.
 constexpr int kTokenMaxRows = 32;
-// Its workers, as many waves as stay resident with their rings of LDS buffers (32 KiB, 64 KiB
-// for more than 128 elements) on 256 compute units of 160 KiB.
-inline int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1280; }
+// Its workers: four waves on each of 256 compute units with 32 KiB of LDS buffers each, two with
+// 64 KiB for more than 128 elements.  (Reads of 1.5 GiB by such waves alone: 6.1 TB/s with four
+// a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
+inline int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);

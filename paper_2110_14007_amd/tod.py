@@ -9,6 +9,7 @@ PyTorch fallback).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -655,24 +656,48 @@ def tod_loci(x, radii, alpha: float = 0.5, n_min: int = 20, k_sigma: float = 3.0
 # sequence operators: queued on the stream, not waited for
 # ---------------------------------------------------------------------------
 
-def _dev_tensor(x, name, dtypes, dim, device=None):
-    torch = _torch()
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+class _Seq:
+    """What the calls below need of torch, looked up once: they queue microseconds of work, and
+    the program's time between two calls counts as much as the GPU's."""
+
+    def __init__(self):
+        torch = _torch()
+        self.f32, self.i32, self.i64 = (torch.float32,), (torch.int32,), (torch.int64,)
+        self.half = (torch.float16, torch.bfloat16)
+        self.fp16 = torch.float16
+        self.stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
+        self.device = torch._C._cuda_getDevice
+        self.guard = torch.cuda.device
+
+
+_seq_env = None
+
+
+def _seq():
+    global _seq_env
+    if _seq_env is None:
+        _seq_env = _Seq()
+    return _seq_env
+
+
+def _index_of(x, name):
+    """Device index of a call's first tensor."""
+    if not isinstance(x, _torch().Tensor) or not x.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) torch tensor" % name)
-    if x.dtype not in dtypes:
-        raise TypeError("%s must have dtype %s" % (name, " or ".join(str(d) for d in dtypes)))
-    if x.dim() != dim:
-        raise TypeError("%s must have %d dimensions" % (name, dim))
-    if device is not None and x.device != device:
-        raise ValueError("%s must be on %s" % (name, device))
-    return x
+    return x.get_device()
 
 
-def _dev_array(x, name, dtype, dim, device=None):
-    _dev_tensor(x, name, (dtype,), dim, device)
-    if not x.is_contiguous():
-        raise TypeError("%s must be contiguous" % name)
-    return x
+def _want(x, name, dtypes, dim, index, contiguous=True):
+    try:
+        if (x.get_device() == index and x.dtype in dtypes and x.dim() == dim
+                and (not contiguous or x.is_contiguous())):
+            return
+    except AttributeError:
+        pass
+    if _index_of(x, name) != index:
+        raise ValueError("%s must be on the other tensors' device" % name)
+    raise TypeError("%s must be a %s%d-dimensional tensor of dtype %s" % (
+        name, "contiguous " if contiguous else "", dim, " or ".join(str(d) for d in dtypes)))
 
 
 def _strides(x, name):
@@ -686,33 +711,33 @@ def _strides(x, name):
     return (row if tokens > 1 else 0), (head if heads > 1 else dim)
 
 
-class _On:
-    """The stream of a call.  Its work outlives the call, and torch's allocator gives freed
-    memory to the stream that it was allocated on: with a stream of the caller's, every tensor
-    of the call is recorded as used there."""
+def _queue(where, fn, index, stream, tensors, *args):
+    """fn(*args, stream pointer, ...) on the stream; args holds None in the stream's place.
 
-    def __init__(self, stream, device):
-        torch = _torch()
-        self.current = torch.cuda.current_stream(device)
-        self.stream = self.current if stream is None else stream
-        if self.stream.device != device:
+    The work outlives the call, and torch's allocator gives freed memory to the stream that it
+    was allocated on: with a stream of the caller's, every tensor is recorded as used there."""
+    env = _seq()
+    current = env.stream(index)
+    at = current
+    if stream is not None:
+        if stream.device.index != index:
             raise ValueError("the stream belongs to another device than the tensors")
-        self.device = device
-        self.ptr = ctypes.c_void_p(self.stream.cuda_stream)
+        at = stream.cuda_stream
+    args = [at if a is _STREAM else a for a in args]
+    if env.device() == index:
+        status = fn(*args)
+    else:
+        with env.guard(index):
+            status = fn(*args)
+    if status != TOD_OK:
+        _check(status, where)
+    if at != current:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
-    def call(self, where, fn, *args):
-        torch = _torch()
-        if torch.cuda.current_device() == self.device.index:
-            _check(fn(*args), where)
-        else:
-            with torch.cuda.device(self.device):
-                _check(fn(*args), where)
 
-    def used(self, *tensors):
-        if self.stream.cuda_stream != self.current.cuda_stream:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+_STREAM = object()
 
 
 def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, stream=None):
@@ -723,92 +748,98 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     -> (row_start int32 [n_seq + 1], slot int64 [tokens], pos int32 [tokens],
         used int64 [2]: pages taken from free_pages, new tokens left without a slot)
     """
-    torch = _torch()
-    _dev_array(cached, "cached", torch.int32, 1)
-    dev, n = cached.device, cached.shape[0]
-    _dev_array(fresh, "fresh", torch.int32, 1, dev)
-    _dev_array(free_pages, "free_pages", torch.int32, 1, dev)
-    _dev_array(table, "table", torch.int32, 2, dev)
-    if fresh.shape[0] != n or table.shape[0] != n:
+    env = _seq()
+    dev = _index_of(cached, "cached")
+    _want(cached, "cached", env.i32, 1, dev)
+    _want(fresh, "fresh", env.i32, 1, dev)
+    _want(free_pages, "free_pages", env.i32, 1, dev)
+    _want(table, "table", env.i32, 2, dev)
+    n, cols = table.shape
+    if fresh.shape[0] != n or cached.shape[0] != n:
         raise ValueError("cached, fresh and table must have one row per sequence")
     tokens = int(tokens)
-    on = _On(stream, dev)
     room = max(tokens, 0)
-    out = torch.empty((2 + room,), dtype=torch.int64, device=dev)
-    rows = torch.empty((n + 1 + room,), dtype=torch.int32, device=dev)
-    used, slot, row_start, pos = out[:2], out[2:], rows[:n + 1], rows[n + 1:]
-    on.call("tod_page_map", _lib.tod_page_map, cached.data_ptr(), fresh.data_ptr(), n,
-            free_pages.data_ptr(), free_pages.shape[0], int(page_rows), table.data_ptr(),
-            table.shape[1], tokens, on.ptr, row_start.data_ptr(), slot.data_ptr(),
-            pos.data_ptr(), used.data_ptr())
-    on.used(cached, fresh, free_pages, table, out, rows)
+    # One allocation: used, slot (int64), then row_start and pos (int32).
+    words = 2 * (2 + room)
+    buf = cached.new_empty((words + n + 1 + room,))
+    longs = buf[:words].view(env.i64[0])
+    used, slot = longs[:2], longs[2:]
+    row_start, pos = buf[words:words + n + 1], buf[words + n + 1:]
+    base = buf.data_ptr()
+    rows = base + 4 * words
+    _queue("tod_page_map", _lib.tod_page_map, dev, stream,
+           (cached, fresh, free_pages, table, buf),
+           cached.data_ptr(), fresh.data_ptr(), n, free_pages.data_ptr(), free_pages.shape[0],
+           int(page_rows), table.data_ptr(), cols, tokens, _STREAM, rows, base + 16,
+           rows + 4 * (n + 1), base)
     return row_start, slot, pos, used
 
 
-def _pages(k_pages, v_pages, dtypes, device):
-    _dev_tensor(k_pages, "k_pages", dtypes, 4, device)
-    _dev_tensor(v_pages, "v_pages", (k_pages.dtype,), 4, device)
+def _pages(k_pages, v_pages, dtypes, index):
+    _want(k_pages, "k_pages", dtypes, 4, index)
+    _want(v_pages, "v_pages", (k_pages.dtype,), 4, index)
     if k_pages.shape != v_pages.shape:
         raise ValueError("k_pages and v_pages must have the same shape")
-    if not k_pages.is_contiguous() or not v_pages.is_contiguous():
-        raise TypeError("k_pages and v_pages must be contiguous")
     return k_pages.shape
 
 
 def tod_page_write(k, v, slot, k_pages, v_pages, stream=None):
     """Write k, v [tokens, kv_heads, dim] into their slots (int64 [tokens], negative: none) of
     k_pages, v_pages [n_pages, kv_heads, page_rows, dim], in place."""
-    torch = _torch()
-    halves = (torch.float16, torch.bfloat16)
-    _dev_tensor(k, "k", halves, 3)
-    dev = k.device
-    _dev_tensor(v, "v", (k.dtype,), 3, dev)
-    _dev_array(slot, "slot", torch.int64, 1, dev)
+    env = _seq()
+    dev = _index_of(k, "k")
+    _want(k, "k", env.half, 3, dev, False)
+    _want(v, "v", (k.dtype,), 3, dev, False)
+    _want(slot, "slot", env.i64, 1, dev)
     n_pages, kv_heads, page_rows, dim = _pages(k_pages, v_pages, (k.dtype,), dev)
     tokens = slot.shape[0]
-    if tuple(k.shape) != (tokens, kv_heads, dim) or v.shape != k.shape:
+    if k.shape != (tokens, kv_heads, dim) or v.shape != k.shape:
         raise ValueError("k and v must be [%d, %d, %d] as slot and the pages are"
                          % (tokens, kv_heads, dim))
-    on = _On(stream, dev)
     (kr, kh), (vr, vh) = _strides(k, "k"), _strides(v, "v")
-    on.call("tod_page_write", _lib.tod_page_write, k.data_ptr(), v.data_ptr(), tokens, kv_heads,
-            dim, kr, kh, vr, vh, slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
-            page_rows, on.ptr)
-    on.used(k, v, slot, k_pages, v_pages)
+    _queue("tod_page_write", _lib.tod_page_write, dev, stream, (k, v, slot, k_pages, v_pages),
+           k.data_ptr(), v.data_ptr(), tokens, kv_heads, dim, kr, kh, vr, vh, slot.data_ptr(),
+           k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_rows, _STREAM)
 
 
-def _attn(q, kv_heads, causal, scale):
-    torch = _torch()
-    a = tod_attn()
-    a.struct_size = ctypes.sizeof(tod_attn)
-    a.precision = PREC_FP16 if q.dtype == torch.float16 else PREC_BF16
-    a.heads, a.kv_heads, a.dim = q.shape[1], kv_heads, q.shape[2]
-    a.causal = int(bool(causal))
-    a.scale = 0.0 if scale is None else float(scale)
-    if scale is not None and not a.scale > 0.0:
+def _attn(q, kv_heads, causal, scale, k=None, v=None):
+    _, heads, dim = q.shape
+    if scale is None:
+        scale = 0.0
+    elif not scale > 0.0:
         raise ValueError("scale must be positive")
-    a.q_row, a.q_head = _strides(q, "q")
-    return a
+    kr = kh = vr = vh = 0
+    if k is not None:
+        (kr, kh), (vr, vh) = _strides(k, "k"), _strides(v, "v")
+    qr, qh = _strides(q, "q")
+    return tod_attn(_ATTN_SIZE, PREC_FP16 if q.dtype == _seq().fp16 else PREC_BF16, heads,
+                    kv_heads, dim, 1 if causal else 0, scale, qr, qh, kr, kh, vr, vh)
+
+
+_ATTN_SIZE = ctypes.sizeof(tod_attn)
 
 
 def _attn_outputs(q, out, return_lse):
-    torch = _torch()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device \
             or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    return out, lse
+    return out, (q.new_empty(q.shape[:2], dtype=_seq().f32[0]) if return_lse else None)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attn_room(heads, kv_heads, dim, tokens, n_seq, max_fresh):
+    a = tod_attn()
+    _lib.tod_default_attn(ctypes.byref(a), heads, kv_heads, dim, PREC_FP16)
+    return int(_lib.tod_attn_workspace_size(ctypes.byref(a), tokens, n_seq, max_fresh))
 
 
 def tod_attn_workspace_size(heads: int, kv_heads: int, dim: int, tokens: int, n_seq: int,
                             max_fresh=None) -> int:
     """Workspace bytes of tod_attn_prompt and tod_attn_paged (0: sizes that they refuse)."""
-    a = tod_attn()
-    _lib.tod_default_attn(ctypes.byref(a), int(heads), int(kv_heads), int(dim), PREC_FP16)
-    return int(_lib.tod_attn_workspace_size(ctypes.byref(a), int(tokens), int(n_seq),
-                                            int(tokens if max_fresh is None else max_fresh)))
+    return _attn_room(int(heads), int(kv_heads), int(dim), int(tokens), int(n_seq),
+                      int(tokens if max_fresh is None else max_fresh))
 
 
 def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspace=None,
@@ -819,27 +850,25 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
     strides that are multiples of 8); row_start int32 [n_seq + 1].
     -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
     """
-    torch = _torch()
-    _dev_tensor(q, "q", (torch.float16, torch.bfloat16), 3)
-    dev = q.device
-    _dev_tensor(k, "k", (q.dtype,), 3, dev)
-    _dev_tensor(v, "v", (q.dtype,), 3, dev)
-    _dev_array(row_start, "row_start", torch.int32, 1, dev)
-    tokens, _, dim = q.shape
-    if k.shape != v.shape or k.shape[0] != tokens or k.shape[2] != dim:
+    env = _seq()
+    dev = _index_of(q, "q")
+    _want(q, "q", env.half, 3, dev, False)
+    _want(k, "k", (q.dtype,), 3, dev, False)
+    _want(v, "v", (q.dtype,), 3, dev, False)
+    _want(row_start, "row_start", env.i32, 1, dev)
+    tokens, heads, dim = q.shape
+    kv_heads, n = k.shape[1], row_start.shape[0] - 1
+    if k.shape != (tokens, kv_heads, dim) or v.shape != k.shape:
         raise ValueError("k and v must be [tokens, kv_heads, dim] with q's tokens and dim")
-    a = _attn(q, k.shape[1], causal, scale)
-    a.k_row, a.k_head = _strides(k, "k")
-    a.v_row, a.v_head = _strides(v, "v")
-    on = _On(stream, dev)
+    a = _attn(q, kv_heads, causal, scale, k, v)
     out, lse = _attn_outputs(q, out, return_lse)
-    n = row_start.shape[0] - 1
-    need = int(_lib.tod_attn_workspace_size(ctypes.byref(a), tokens, n, tokens))
-    wsbuf, wsp, wsn = _ws(workspace, need, dev)
-    on.call("tod_attn_prompt", _lib.tod_attn_prompt, ctypes.byref(a), q.data_ptr(), k.data_ptr(),
-            v.data_ptr(), tokens, row_start.data_ptr(), n, wsp, wsn, on.ptr, out.data_ptr(),
-            lse.data_ptr() if return_lse else None)
-    on.used(q, k, v, row_start, out, lse, wsbuf)
+    buf, ws, ws_bytes = _ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens),
+                            q.device)
+    _queue("tod_attn_prompt", _lib.tod_attn_prompt, dev, stream,
+           (q, k, v, row_start, out, lse, buf),
+           ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens,
+           row_start.data_ptr(), n, ws, ws_bytes, _STREAM, out.data_ptr(),
+           lse.data_ptr() if return_lse else None)
     return (out, lse) if return_lse else out
 
 
@@ -853,29 +882,29 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
     where the caller knows it.
     -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
     """
-    torch = _torch()
-    _dev_tensor(q, "q", (torch.float16, torch.bfloat16), 3)
-    dev = q.device
+    env = _seq()
+    dev = _index_of(q, "q")
+    _want(q, "q", env.half, 3, dev, False)
     n_pages, kv_heads, page_rows, dim = _pages(k_pages, v_pages, (q.dtype,), dev)
-    _dev_array(table, "table", torch.int32, 2, dev)
-    _dev_array(row_start, "row_start", torch.int32, 1, dev)
-    _dev_array(cached, "cached", torch.int32, 1, dev)
-    tokens, n = q.shape[0], cached.shape[0]
+    _want(table, "table", env.i32, 2, dev)
+    _want(row_start, "row_start", env.i32, 1, dev)
+    _want(cached, "cached", env.i32, 1, dev)
+    tokens, heads, _ = q.shape
+    n, cols = table.shape
     if q.shape[2] != dim:
         raise ValueError("q and the pages must have the same dim")
-    if table.shape[0] != n or row_start.shape[0] != n + 1:
+    if cached.shape[0] != n or row_start.shape[0] != n + 1:
         raise ValueError("table, row_start and cached must describe the same sequences")
     a = _attn(q, kv_heads, True, scale)
-    on = _On(stream, dev)
     out, lse = _attn_outputs(q, out, return_lse)
     fresh = tokens if max_fresh is None else int(max_fresh)
-    need = int(_lib.tod_attn_workspace_size(ctypes.byref(a), tokens, n, fresh))
-    wsbuf, wsp, wsn = _ws(workspace, need, dev)
-    on.call("tod_attn_paged", _lib.tod_attn_paged, ctypes.byref(a), q.data_ptr(),
-            k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_rows, table.data_ptr(),
-            table.shape[1], row_start.data_ptr(), cached.data_ptr(), n, tokens, fresh, wsp, wsn,
-            on.ptr, out.data_ptr(), lse.data_ptr() if return_lse else None)
-    on.used(q, k_pages, v_pages, table, row_start, cached, out, lse, wsbuf)
+    buf, ws, ws_bytes = _ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh),
+                            q.device)
+    _queue("tod_attn_paged", _lib.tod_attn_paged, dev, stream,
+           (q, k_pages, v_pages, table, row_start, cached, out, lse, buf),
+           ctypes.byref(a), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
+           page_rows, table.data_ptr(), cols, row_start.data_ptr(), cached.data_ptr(), n, tokens,
+           fresh, ws, ws_bytes, _STREAM, out.data_ptr(), lse.data_ptr() if return_lse else None)
     return (out, lse) if return_lse else out
 
 
