@@ -56,24 +56,32 @@ __device__ __forceinline__ int32_t start_of(const AttnArgs& a, int32_t s) {
   return s <= 0 ? 0 : min(max(a.row_start[s], 0), a.tokens);
 }
 
+// From the sequence's row_start, the next one's and its cached tokens.
 template <bool PAGED>
-__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int32_t s) {
+__device__ __forceinline__ Seq make_seq(const AttnArgs& a, int32_t s, int32_t start, int32_t next,
+                                        int32_t cached) {
   Seq q;
-  q.start = start_of(a, s);
-  const int32_t end = s < a.n_seq ? max(start_of(a, s + 1), q.start) : a.tokens;
-  q.n = end - q.start;
+  q.start = start;
+  q.n = (s < a.n_seq ? max(next, start) : a.tokens) - start;
   q.shift = 0;
   q.keys = 0;
   if (s < a.n_seq) {
     if constexpr (PAGED) {
-      const int32_t room = (int32_t)(a.cols * a.page.d);
-      q.shift = min(max(a.cached[s], 0), room);
+      const int32_t room = (int32_t)a.cols * (int32_t)a.page.d;
+      q.shift = min(max(cached, 0), room);
       q.keys = min(q.shift + q.n, room);
     } else {
       q.keys = q.n;
     }
   }
   return q;
+}
+
+template <bool PAGED>
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int32_t s) {
+  const bool real = s < a.n_seq;
+  return make_seq<PAGED>(a, s, start_of(a, s), real ? start_of(a, s + 1) : 0,
+                         PAGED && real ? a.cached[s] : 0);
 }
 
 // 16 zero bytes: what a lane stages for a key, or a piece of one, that does not exist.
@@ -144,6 +152,7 @@ struct Stager {
       if (lo < first || hi - first >= 64) {
         first = lo;
         entry = lo + lane < a.cols ? a.table[(int64_t)seq * a.cols + lo + lane] : -1;
+        asm volatile("" : "+v"(entry));  // waited for here, not by every stage's first use
       }
       const uint32_t pg = div_by((uint32_t)j, a.page);
       const int32_t id = __shfl(entry, (int)(pg - (uint32_t)first) & 63, 64);
@@ -153,6 +162,22 @@ struct Stager {
     } else {
       return j < seen ? (uint32_t)(start + j) : ~0u;
     }
+  }
+
+  // Row of the cache of key j, the same for the whole wave; ~0: none.  The window of entries
+  // begins a little before it, for the values that are staged after their keys.
+  __device__ __forceinline__ uint32_t row_of(int32_t j) {
+    const int32_t pg = (int32_t)div_by((uint32_t)j, a.page);
+    if (pg < first || pg - first >= 64) {
+      first = max(pg - 16, 0);
+      const int32_t e = first + (int32_t)(threadIdx.x & 63);
+      entry = e < a.cols ? a.table[(int64_t)seq * a.cols + e] : -1;
+      asm volatile("" : "+v"(entry));  // waited for here, not by every stage's first use
+    }
+    const int32_t id = __builtin_amdgcn_readlane(entry, pg - first);
+    if (id < 0 || id >= a.n_pages) return ~0u;
+    return ((uint32_t)id * (uint32_t)a.kv_heads + head) * a.page.d +
+           ((uint32_t)j - (uint32_t)pg * a.page.d);
   }
 
   // Rows r0 .. r0 + kRowsLoad - 1 of a K (or V) stage that begins at LDS address `to`.
@@ -197,14 +222,23 @@ struct Stager {
   }
 };
 
-// Query operand: elements 16 c + 8 h .. + 7 of row p, zero from dim on.
+// Query operand: elements 16 c + 8 h .. + 7 of row p, zero from dim on.  Every lane loads (from the
+// row's start where there is nothing): with a branch around each, the loads would run one by one.
 template <typename ET, int DP>
 __device__ __forceinline__ void load_query(typename Frag<ET>::V (&q)[DP / 16], const ET* p,
                                            int32_t dim, int h) {
+  u32x4 w[DP / 16];
 #pragma unroll
   for (int c = 0; c < DP / 16; ++c) {
     const int e = 16 * c + 8 * h;
-    q[c] = e < dim ? *(const typename Frag<ET>::V*)(p + e) : typename Frag<ET>::V{};
+    w[c] = *(const u32x4*)(p + (e < dim ? e : 0));
+  }
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) {
+    const bool in = 16 * c + 8 * h < dim;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[c][i] = in ? w[c][i] : 0u;
+    q[c] = __builtin_bit_cast(typename Frag<ET>::V, w[c]);
   }
 }
 
@@ -250,22 +284,33 @@ __device__ __forceinline__ float log_sum(float m, float sum) {
   return sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// O^T accumulators of row l % 32 times f, as the output type, into its row at p.
+// O^T accumulators of a wave's 32 rows, row l % 32 times f, as the output type into the rows at
+// out: rows that lie at the lanes' element offsets `at` (below 0: no such row).  They pass through
+// the wave's own 32 x DP elements of LDS at `lds`, so that each store writes whole rows: from
+// the accumulators a lane could write 8 bytes at a time only.
 template <typename ET, int DP>
-__device__ __forceinline__ void store_row(const f32x16 (&o)[DP / 32], float f, ET* p, int32_t dim,
-                                          int h) {
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[DP / 32], float f, ET* out, int64_t at,
+                                           int32_t dim, uint16_t* lds) {
+  constexpr int kPieces = DP / 8, kRowsStore = 64 / kPieces;  // 16-byte pieces; rows of a store
+  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int e = 32 * d + 8 * g + 4 * h;
-      if (e < dim) {
-        uint2 w;
-        w.x = pack2<ET>(o[d][4 * g] * f, o[d][4 * g + 1] * f);
-        w.y = pack2<ET>(o[d][4 * g + 2] * f, o[d][4 * g + 3] * f);
-        *(uint2*)(p + e) = w;
-      }
+      uint2 w;
+      w.x = pack2<ET>(o[d][4 * g] * f, o[d][4 * g + 1] * f);
+      w.y = pack2<ET>(o[d][4 * g + 2] * f, o[d][4 * g + 3] * f);
+      const int piece = (4 * d + g) ^ swizzle_k<DP>(col);
+      *(uint2*)(lds + col * DP + 8 * piece + 4 * h) = w;
     }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32 / kRowsStore; ++i) {
+    const int row = i * kRowsStore + lane / kPieces, piece = lane % kPieces;
+    const u32x4 w = *(const u32x4*)(lds + row * DP + 8 * (piece ^ swizzle_k<DP>(row)));
+    const int64_t to = __shfl(at, row, 64);
+    if (to >= 0 && 8 * piece < dim) *(u32x4*)(out + to + 8 * piece) = w;
+  }
 }
 
 // The same, unscaled fp32, into a row of a split's partial result.

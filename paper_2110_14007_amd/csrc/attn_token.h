@@ -226,17 +226,15 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
     }
     sum += other_half(sum);
 
-    if (col < rows) {
-      if (jb == 0 && je == stages) {
-        const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
-        store_row<ET, DP>(o, inverse(sum), (ET*)a.out + orow * a.dim, a.dim, h);
-        if (a.lse && h == 0) a.lse[orow] = log_sum(mref, sum);
-      } else {
-        // At most two of a worker's pieces are not whole: its first and its last.
-        const int64_t row = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows + col;
-        store_part<DP>(o, a.token_o + row * DP, h);
-        if (h == 0) a.token_stat[row] = {mref, sum};
-      }
+    if (jb == 0 && je == stages) {
+      const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
+      if (a.lse && h == 0 && col < rows) a.lse[orow] = log_sum(mref, sum);
+      store_rows<ET, DP>(o, inverse(sum), (ET*)a.out, col < rows ? orow * a.dim : -1, a.dim, lds);
+    } else if (col < rows) {
+      // At most two of a worker's pieces are not whole: its first and its last.
+      const int64_t row = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows + col;
+      store_part<DP>(o, a.token_o + row * DP, h);
+      if (h == 0) a.token_stat[row] = {mref, sum};
     }
     // Its stores and LDS reads are done before the next pair's loads are counted.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");

@@ -57,7 +57,7 @@ struct AttnArgs {
   FastDiv page, group;  // rows of a page; query heads per key / value head
   int32_t heads, kv_heads, dim;
   int32_t causal;
-  float scale;  // of q k^T, times log2(e)
+  float scale, unscale;  // of q k^T, times log2(e), and its inverse
   void* out;
   float* lse;
   // Sequences of at most skip_rows packed rows are the token kernel's (0: none).
@@ -66,9 +66,10 @@ struct AttnArgs {
   float2* token_stat;   // [2 workers, skip_rows]
   float* token_o;       // [2 workers, skip_rows, padded dim]
   // Splits of a tile's keys.
-  int32_t tile_rows;    // rows of a tile
-  int32_t tile_parts;   // most splits of one
-  int32_t part_stages;  // fewest stages (of 64 keys) of a split
+  int32_t tile_slots;   // of a key / value head
+  int32_t tile_parts;   // most splits of a tile
+  FastDiv parts_div, heads_div;  // by tile_parts and kv_heads
+  int32_t part_keys;    // fewest keys of a split
   float2* tile_stat;    // [tiles of all heads, parts, rows]
   float* tile_o;        // [tiles of all heads, parts, rows, padded dim]
 };

@@ -3,7 +3,6 @@
 // HIP graph.
 #include <math.h>
 #include <stdio.h>
-#include <stdlib.h>
 #include <string.h>
 
 #include "seq.h"
@@ -13,6 +12,7 @@ namespace {
 using tod::set_error;
 
 constexpr int64_t kMaxCount = 0x7fffffffLL;
+constexpr int32_t kPartKeys = 512;  // fewest keys of a split of a tile
 
 tod_status invalid(const char* msg) { return set_error(TOD_ERR_INVALID_ARG, msg); }
 tod_status unsupported(const char* msg) { return set_error(TOD_ERR_UNSUPPORTED, msg); }
@@ -92,14 +92,17 @@ void fill(const tod_attn& o, tod::AttnArgs* a) {
   a->kv_heads = o.kv_heads;
   a->dim = o.dim;
   a->group = tod::fast_div((uint32_t)(o.heads / o.kv_heads));
+  a->heads_div = tod::fast_div((uint32_t)o.kv_heads);
   a->page = tod::fast_div(1);
   a->causal = o.causal;
   a->scale = o.scale * 1.44269504088896341f;
+  a->unscale = 1.0f / a->scale;
 }
 
 // Workspace of a call, and how its work is split.
 struct Plan {
-  int32_t skip_rows, tile_rows, tile_parts, part_stages;
+  int32_t skip_rows, tile_parts;
+  int64_t tile_slots;
   bool tile;  // some sequence may have more rows than the token kernel takes
   size_t line, token_stat, token_o, tile_stat, tile_o, total;
 };
@@ -125,24 +128,20 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
     p.token_stat = take(rows * 8);
     p.token_o = take(rows * dp * 4);
   }
-  p.tile_rows = 128;
   p.tile_parts = 1;
-  p.part_stages = 8;
+  p.tile_slots = tokens * group / 128 + n_seq + 1;
   if (p.tile) {
-    const int64_t wide = (tokens * group + 255) / 256 * o.kv_heads;
-    const int kw = getenv("KW") ? atoi(getenv("KW")) : 512, kp = getenv("KP") ? atoi(getenv("KP")) : 1024, km = getenv("KM") ? atoi(getenv("KM")) : 8;
-    if (o.dim <= 128 && wide >= kw) p.tile_rows = 256;
-    const int64_t tiles = (tokens * group + p.tile_rows - 1) / p.tile_rows * o.kv_heads;
-    const int64_t slots = (tokens * group / p.tile_rows + n_seq + 1) * o.kv_heads;
-    const int64_t parts = kp / tiles;
-    p.part_stages = km;
-    p.tile_parts = (int32_t)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
-    // A prompt has no more keys than tokens; a split has at least 512.
-    if (!paged && p.tile_parts > tokens / 512) p.tile_parts = tokens < 1024 ? 1 : (int32_t)(tokens / 512);
-    while (p.tile_parts > 1 && slots * p.tile_parts * p.tile_rows > 2048 * 128) --p.tile_parts;
+    // Two workgroups on every compute unit, from the rows that there are; slots beside them stay
+    // empty.  A prompt has no more keys than tokens; a split has at least 512.
+    const int64_t tiles = (tokens * group + 127) / 128 * o.kv_heads;
+    const int64_t slots = p.tile_slots * o.kv_heads;
+    int64_t parts = 512 / tiles;
+    if (!paged && parts > tokens / kPartKeys) parts = tokens / kPartKeys;
+    while (parts > 1 && (parts > 16 || slots * parts > 2048)) --parts;
+    p.tile_parts = (int32_t)(parts < 1 ? 1 : parts);
     if (p.tile_parts > 1) {
-      p.tile_stat = take(slots * p.tile_parts * p.tile_rows * 8);
-      p.tile_o = take(slots * p.tile_parts * p.tile_rows * dp * 4);
+      p.tile_stat = take(slots * p.tile_parts * 128 * 8);
+      p.tile_o = take(slots * p.tile_parts * 128 * dp * 4);
     }
   }
   p.total = at ? at : 256;
@@ -160,9 +159,10 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool pag
   a->token_line = (int64_t*)(base + p.line);
   a->token_stat = (float2*)(base + p.token_stat);
   a->token_o = (float*)(base + p.token_o);
-  a->tile_rows = p.tile_rows;
+  a->tile_slots = (int32_t)p.tile_slots;
   a->tile_parts = p.tile_parts;
-  a->part_stages = p.part_stages;
+  a->parts_div = tod::fast_div((uint32_t)p.tile_parts);
+  a->part_keys = kPartKeys;
   a->tile_stat = (float2*)(base + p.tile_stat);
   a->tile_o = (float*)(base + p.tile_o);
   const hipStream_t s = (hipStream_t)stream;
