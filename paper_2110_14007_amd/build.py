@@ -26,6 +26,10 @@ NO_NAN_SOURCES = {"mtile_f16.hip", "mtile_bf16.hip", "tile_f32.hip", "tile_f16.h
                   # sums carry them to the output; nothing compares them with themselves.)
                   "attn_tile_f16.hip", "attn_tile_bf16.hip", "attn_token_f16.hip",
                   "attn_token_bf16.hip"}
+# The attention kernels keep their accumulators in VGPRs (the softmax works on them between two
+# products): left to itself the compiler puts the MFMA results of a kernel that needs more than
+# 256 registers in AGPRs and copies every score and rescaled accumulator.
+VGPR_FORM_SOURCES = {s for s in SOURCES if s.startswith("attn_")}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [
@@ -43,6 +47,8 @@ def build(verbose: bool = False) -> str:
     def compile_one(src: str) -> str:
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
         extra = ["-fno-honor-nans"] if src in NO_NAN_SOURCES else []
+        if src in VGPR_FORM_SOURCES:
+            extra += ["-mllvm", "-amdgpu-mfma-vgpr-form"]
         cmd = [HIPCC, *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         out = "\n".join(line for line in (r.stdout + r.stderr).splitlines()

@@ -275,13 +275,83 @@ __device__ __forceinline__ typename Frag<ET>::V values(const uint16_t* vs, int r
                             __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 1 / sum, 0 for a row without keys; a NaN sum stays one.
-__device__ __forceinline__ float inverse(float sum) {
-  return sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+// Whether a V stage of 32 keys holds an infinity or a NaN, the same for the whole wave.
+template <typename ET, int DP>
+__device__ __forceinline__ bool holds_nonfinite(const uint16_t* vs) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 32 * DP / 512; ++i) {
+    const u32x4 v = *(const u32x4*)(vs + 8 * (64 * i + (threadIdx.x & 63)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu));
+  }
+  return __ballot(top[0] >= kInf || top[1] >= kInf) != 0;
 }
 
+// Clears those of the stage's values, the thread's share of it (from first, every step threads).
+template <typename ET, int DP>
+__device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int step) {
+  constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
+  for (int i = first + (threadIdx.x & 63); i < 32 * DP; i += step)
+    if ((vs[i] & 0x7fff) >= kInf) vs[i] = 0;
+}
+
+// After the stores of a wave's 32 packed rows from m0 on: where a row sees values that are not
+// finite among the keys j0 .. j1 - 1, they are added to its output (the weights are positive).  step 0: rows of the output; else partial results
+// of the rows one after the other, step elements each.
+template <typename ET, int DP, bool PAGED, typename OT, typename ST>
+__device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step, const Seq& s,
+                                                  int32_t m0, int32_t j0, int32_t j1) {
+  const AttnArgs& a = st.a;
+  const int lane = threadIdx.x & 63;
+  constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores that this one follows
+#pragma unroll 1
+  for (int32_t r = 0; r < 32; ++r) {
+    const int32_t m = m0 + r;
+    if (m >= s.n * (int32_t)a.group.d) break;
+    const int32_t tok = (int32_t)div_by((uint32_t)m, a.group);
+    const int32_t end = min(min(s.shift + tok + 1, s.keys), j1);
+    const int64_t row = (int64_t)(s.start + tok) * a.heads +
+                        (int64_t)st.head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
+    OT* const to = step ? out + (int64_t)r * step : out + row * a.dim;
+#pragma unroll 1
+    for (int32_t e = lane; e < a.dim; e += 64) {
+      float sum = 0.0f;
+      bool any = false;
+#pragma unroll 1
+      for (int32_t j = j0; j < end; ++j) {
+        const ET* p = (const ET*)a.v;
+        if constexpr (PAGED) {
+          const uint32_t pg = div_by((uint32_t)j, a.page);
+          const int32_t id = a.table[(int64_t)st.seq * a.cols + pg];
+          if (id < 0 || id >= a.n_pages) continue;
+          p += (((int64_t)id * a.kv_heads + st.head) * a.page.d + (j - (int32_t)(pg * a.page.d))) *
+               a.dim;
+        } else {
+          p += (int64_t)(s.start + j) * a.v_row + (int64_t)st.head * a.v_head;
+        }
+        const uint16_t u = ((const uint16_t*)p)[e];
+        if ((u & 0x7fff) >= kInf) {
+          any = true;
+          sum += (float)__builtin_bit_cast(ET, u);
+        }
+      }
+      if (any) to[e] = (OT)((float)to[e] + sum);  // (still NaN where the weights are)
+    }
+  }
+}
+
+// What a row's O is multiplied by, and its log sum.  A row without keys has the sum 0 and O = 0:
+// its output is 0 and its log sum -inf without a test for it (a comparison would not do: these
+// files are compiled as if none met a NaN, and where a score is NaN the sum and O are).
+__device__ __forceinline__ float inverse(float sum) { return 1.0f / fmaxf(sum, 1.17549435e-38f); }
+
 __device__ __forceinline__ float log_sum(float m, float sum) {
-  return sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+  return (m + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // O^T accumulators of a wave's 32 rows, row l % 32 times f, as the output type into the rows at

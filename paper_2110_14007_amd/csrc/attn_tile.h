@@ -84,7 +84,7 @@ __device__ __forceinline__ const void* uniform(const void* p) {
 }
 
 template <typename ET, int DP, bool PAGED>
-__global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3) tile_kernel(AttnArgs a) {
   using V8 = typename Frag<ET>::V;
   using St = Stager<ET, DP, PAGED>;
   constexpr int kStage = kKeys * DP;         // elements of a stage
@@ -108,7 +108,10 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
   const int32_t tok = (int32_t)div_by((uint32_t)m, a.group);
   const int32_t qh = (int32_t)head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
   const int32_t limit = PAGED || a.causal ? min(t.shift + tok, t.keys - 1) : t.keys - 1;
-  const int32_t wlo = __builtin_amdgcn_readfirstlane(limit);
+  // Stages (of this split's) whose keys every row of the tile sees.
+  const int32_t tok0 = (int32_t)div_by((uint32_t)t.row0, a.group);
+  const int32_t least = PAGED || a.causal ? min(t.shift + tok0, t.keys - 1) : t.keys - 1;
+  const int32_t open = min(max((least + 1) / kKeys - jb, 0), count);
   V8 q[KC];
   load_query<ET, DP>(q, (const ET*)a.q + (int64_t)(t.start + tok) * a.q_row + (int64_t)qh * a.q_head,
                      a.dim, h);
@@ -145,11 +148,11 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
     vb = (const ET*)uniform((const ET*)a.v + (int64_t)(t.start + first) * a.v_row +
                             (int64_t)head * a.v_head);
   }
-  // Stage i of this split's into buffer BUF; each of K and V in turn from 0 on.
-  auto stage = [&](auto ISK, int32_t i, auto BUF) __attribute__((always_inline)) {
+  // Stage i of this split's into buffer `ring`; each of K and V in turn from 0 on.
+  auto stage = [&](auto ISK, int32_t i, int ring) __attribute__((always_inline)) {
     constexpr bool isk = decltype(ISK)::value;
     if (i >= count) return;
-    constexpr uint32_t buf = 2u * kStage * (decltype(BUF)::value + (isk ? 0 : kRing));
+    const uint32_t buf = 2u * kStage * (uint32_t)(ring + (isk ? 0 : kRing));
     uint32_t row = 0;
     if constexpr (PAGED) row = i < fast ? st.row_of(first + i * kKeys) : ~0u;
     if (PAGED ? row != ~0u : i < fast) {
@@ -217,9 +220,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
   // ring).  The three do not depend on each other.  They are laid out in slots of one MFMA, the
   // LDS reads of the MFMA kAhead slots on, and a share of the exponentials.
   constexpr int kSlots = KC + 2 * DB, kAhead = 4, kCheck = 2;
-  auto step = [&](int32_t j0, auto KAT, auto VAT, f32x16& s, f32x16& n, const u32x4 (&p0)[2],
-                  u32x4 (&pn)[2]) __attribute__((always_inline)) {
-    constexpr int kat = decltype(KAT)::value, vat = decltype(VAT)::value;
+  auto step = [&](int32_t j0, int kat, int vat, f32x16& s, f32x16& n,
+                  const u32x4 (&p0)[2], u32x4 (&pn)[2]) __attribute__((always_inline)) {
     u32x4 p[2] = {p0[0], p0[1]};
     V8 fr[kSlots];
     auto read = [&](auto I) __attribute__((always_inline)) {
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
         fr[i] = vfrag(vat + 16 * ((i - KC) / DB) * DP * 2, (i - KC) % DB);
     };
     mt::static_for<0, kAhead>([&](auto I) __attribute__((always_inline)) { read(I); });
-    if (j0 + 31 > wlo) {
+    if (j0 + kKeys - 1 > least) {
       const int32_t left = limit - j0 - 4 * h;
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -292,49 +294,62 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
   };
 
   constexpr int kS = 2 * kStage;  // bytes of a stage
+  // Values that some rows of the tile do not see meet their zero weights in the second product,
+  // which is no zero where a value is not finite.  Those values are cleared in their stage (of
+  // index i), and what they make of the rows that do see them is restored at the end.
+  bool cleared = false;
+  auto clear = [&](int32_t i) __attribute__((always_inline)) {
+    if (!(PAGED || a.causal)) return;
+    uint16_t* const vs = lds + (kRing + i % kRing) * kStage;
+    if (!holds_nonfinite<ET, DP>(vs)) return;
+    cleared = true;
+    mt::stage_barrier();
+    clear_nonfinite<ET, DP>(vs, wave * 64, kWaves * 64);
+    mt::stage_barrier();
+  };
   f32x16 sa, sb;
   u32x4 pa[2], pb[2];
   pb[0] = pb[1] = u32x4{0, 0, 0, 0};
-  stage(kIsK, 0, std::integral_constant<int, 0>{});
-  stage(kIsK, 1, std::integral_constant<int, 1>{});
-  stage(kIsV, 0, std::integral_constant<int, 0>{});
-  stage(kIsK, 2, std::integral_constant<int, 2>{});
+  stage(kIsK, 0, 0);
+  stage(kIsK, 1, 1);
+  stage(kIsV, 0, 0);
+  stage(kIsK, 2, 2);
   mt::dl_barrier<0>();
 #pragma unroll
   for (int r = 0; r < 16; ++r) sa[r] = 0.0f;
 #pragma unroll
   for (int c = 0; c < KC; ++c) sa = mfma<ET>(kfrag(0, c), q[c], sa);
-  auto turn = [&](int32_t j, auto R, f32x16& s, f32x16& n, const u32x4 (&p)[2], u32x4 (&pn)[2])
-      __attribute__((always_inline)) {
-    constexpr int r = decltype(R)::value;  // j % kRing
+  auto turn = [&](int32_t j, int r, f32x16& s, f32x16& n, const u32x4 (&p)[2],
+                  u32x4 (&pn)[2]) __attribute__((always_inline)) {  // r: j % kRing
     // The loads of the turn before stay in flight while there are as many as a turn issues.
     if (j + 2 < count)
       mt::dl_barrier<2 * kLoads>();
     else
       mt::dl_barrier<0>();
-    stage(kIsK, j + 3, std::integral_constant<int, (r + 3) % kRing>{});
-    stage(kIsV, j + 1, std::integral_constant<int, (r + 1) % kRing>{});
-    step((jb + j) * 32, std::integral_constant<int, (r + 1) % kRing * kS>{},
-         std::integral_constant<int, (r + kRing - 1) % kRing * kS>{}, s, n, p, pn);
+    stage(kIsK, j + 3, (r + 3) % kRing);
+    stage(kIsV, j + 1, (r + 1) % kRing);
+    if (j > open) clear(j - 1);
+    step((jb + j) * kKeys, (r + 1) % kRing * kS, (r + kRing - 1) % kRing * kS, s, n, p, pn);
   };
   // Scores and weights change places every turn: a pass of the loop takes an even number.
   for (int32_t j = 0; j < count; j += 4) {
-    turn(j, std::integral_constant<int, 0>{}, sa, sb, pb, pa);
+    turn(j, 0, sa, sb, pb, pa);
     if (j + 1 >= count) break;
-    turn(j + 1, std::integral_constant<int, 1>{}, sb, sa, pa, pb);
+    turn(j + 1, 1, sb, sa, pa, pb);
     if (j + 2 >= count) break;
-    turn(j + 2, std::integral_constant<int, 2>{}, sa, sb, pb, pa);
+    turn(j + 2, 2, sa, sb, pb, pa);
     if (j + 3 >= count) break;
-    turn(j + 3, std::integral_constant<int, 3>{}, sb, sa, pa, pb);
+    turn(j + 3, 3, sb, sa, pa, pb);
   }
   if (count > 0) {
+    if (count > open) clear(count - 1);
     const int at = (count - 1) % kRing * kS;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const V8 p = __builtin_bit_cast(V8, count % 2 ? pa[c] : pb[c]);
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] = mfma<ET>(vfrag(at + 16 * c * DP * 2, d), p, o[d]);
-    }
+      for (int d = 0; d < DB; ++d)
+        o[d] = mfma<ET>(vfrag(at + 16 * c * DP * 2, d),
+                        __builtin_bit_cast(V8, count % 2 ? pa[c] : pb[c]), o[d]);
   }
   sum += other_half(sum);
   const bool mine = t.row0 + 32 * wave + col < t.rows;
@@ -342,6 +357,9 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
     const int64_t row = ((int64_t)b * a.tile_parts + part) * kRows + 32 * wave + col;
     if (mine) store_part<DP>(o, a.tile_o + row * DP, h);
     if (mine && h == 0) a.tile_stat[row] = {mref, sum};
+    if (cleared)
+      restore_nonfinite<ET, DP, PAGED>(st, a.tile_o + (row - col) * DP, DP, t, t.row0 + 32 * wave,
+                                       (jb + open) * kKeys, (jb + count) * kKeys);
     return;
   }
   const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
@@ -349,6 +367,9 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : 2) tile_kernel(Att
   mt::stage_barrier();  // the other waves' reads of the stages are done
   store_rows<ET, DP>(o, inverse(sum), (ET*)a.out, mine ? orow * a.dim : -1, a.dim,
                      lds + wave * 32 * DP);
+  if (cleared)
+    restore_nonfinite<ET, DP, PAGED>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, (jb + open) * kKeys,
+                                     (jb + count) * kKeys);
 }
 
 // Joins the splits of a tile, one wave a row.

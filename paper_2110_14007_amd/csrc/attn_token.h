@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     float mref = kNoMax, sum = 0.0f;
+    int32_t cleared = -1;  // from here on values that are not finite were taken for 0
 
     for (int32_t j = jb; j < je; ++j) {
       if (j + kRing <= je)
@@ -202,6 +203,11 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
         x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -mref));
         sum += x[r];
       }
+      // A value that is not finite must not meet the zero weight of a row that does not see it.
+      if (j0 + kTokenKeys - 1 > wlo && rows > (int32_t)a.group.d && holds_nonfinite<ET, DP>(vs)) {
+        clear_nonfinite<ET, DP>(lds + 2 * kStage * ((j - jb) % kRing) + kStage, 0, 64);
+        if (cleared < 0) cleared = j0;
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         typedef ET e8 __attribute__((ext_vector_type(8)));
@@ -230,11 +236,18 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
       const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
       if (a.lse && h == 0 && col < rows) a.lse[orow] = log_sum(mref, sum);
       store_rows<ET, DP>(o, inverse(sum), (ET*)a.out, col < rows ? orow * a.dim : -1, a.dim, lds);
-    } else if (col < rows) {
+      if (cleared >= 0)
+        restore_nonfinite<ET, DP, true>(st, (ET*)a.out, 0, sq, 0, cleared, sq.keys);
+    } else {
       // At most two of a worker's pieces are not whole: its first and its last.
-      const int64_t row = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows + col;
-      store_part<DP>(o, a.token_o + row * DP, h);
-      if (h == 0) a.token_stat[row] = {mref, sum};
+      const int64_t row0 = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows;
+      if (col < rows) {
+        store_part<DP>(o, a.token_o + (row0 + col) * DP, h);
+        if (h == 0) a.token_stat[row0 + col] = {mref, sum};
+      }
+      if (cleared >= 0)
+        restore_nonfinite<ET, DP, true>(st, a.token_o + row0 * DP, DP, sq, 0, cleared,
+                                        je * kTokenKeys);
     }
     // Its stores and LDS reads are done before the next pair's loads are counted.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");

@@ -355,6 +355,82 @@ def test_attn_paged_entries_that_are_no_page(env):
 
 
 # ---------------------------------------------------------------------------
+# infinities and NaN in places that a row does not see
+# ---------------------------------------------------------------------------
+
+HIDDEN = {
+    "prompt": dict(cached=[0], fresh=[200], hq=4, hk=2, d=64),
+    "prompt_long_d128": dict(cached=[0, 0], fresh=[330, 75], hq=2, hk=2, d=128),
+    "prompt_d256": dict(cached=[0], fresh=[90], hq=2, hk=1, d=256),
+    "pages": dict(cached=[150, 0], fresh=[100, 77], hq=4, hk=2, d=128, page=16),
+    "pages_odd": dict(cached=[61], fresh=[90], hq=2, hk=1, d=80, page=7),
+    "few_new": dict(cached=[130, 63], fresh=[4, 3], hq=8, hk=2, d=128, page=32),
+    "few_new_long": dict(cached=[9000], fresh=[5], hq=4, hk=1, d=64, page=16),
+    "split_chunk": dict(cached=[3000], fresh=[40], hq=8, hk=2, d=128, page=16),
+}
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("name", sorted(HIDDEN))
+def test_attn_hidden_nonfinite(env, name, dt):
+    # One of the new tokens has keys that are NaN and values with infinities and NaN.  The rows
+    # before it do not see them; the rows from it on have NaN weights.  Then finite keys with such
+    # values: the rows from it on get infinities and NaN in those columns and no others.
+    torch, tod = env
+    c = HIDDEN[name]
+    paged = "page" in c
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    hq, hk, d, t = c["hq"], c["hk"], c["d"], sum(c["fresh"])
+    starts = starts_of(torch, c["fresh"])
+    at = 2 * c["fresh"][0] // 3  # the token, of the first sequence
+    if paged:
+        q, kp, vp, table = paged_case(torch, c, dt)
+        p = c["cached"][0] + at
+        where = (int(table[0, p // c["page"]]), slice(None), p % c["page"])
+        want, want_lse = paged_want(c, q, kp, vp, table)
+
+        def run(kx, vx):
+            return tod.tod_attn_paged(
+                q, kx, vx, torch.from_numpy(table).cuda(), starts,
+                torch.tensor(c["cached"], dtype=torch.int32, device="cuda"),
+                max_fresh=max(c["fresh"]), return_lse=True)
+    else:
+        q, kp, vp = (rows(torch, gen, dt, t, n, d) for n in (hq, hk, hk))
+        where = (at,)
+        q64, k64, v64 = (x.double().cpu().numpy() for x in (q, kp, vp))
+        want, want_lse, b = np.zeros(q64.shape), np.zeros(q64.shape[:2]), 0
+        for n in c["fresh"]:
+            r = slice(b, b + n)
+            want[r], want_lse[r] = plain_attention(q64[r], k64[r], v64[r], 0, True)
+            b += n
+
+        def run(kx, vx):
+            return tod.tod_attn_prompt(q, kx, vx, starts, return_lse=True)
+
+    v_max = float(vp.abs().max())
+    kx, vx = kp.clone(), vp.clone()
+    vx[where + (Ellipsis, 1)] = float("nan")
+    vx[where + (Ellipsis, 4)] = float("inf")
+    vx[where + (Ellipsis, d - 1)] = -float("inf")
+    out, lse = run(kx, vx)
+    hit = np.zeros(t, bool)
+    hit[at:c["fresh"][0]] = True
+    hit = torch.from_numpy(hit).cuda()
+    o = out.float()
+    assert torch.isnan(o[hit][..., 1]).all()
+    assert (o[hit][..., 4] == math.inf).all() and (o[hit][..., d - 1] == -math.inf).all()
+    fine = o.clone()
+    w = torch.from_numpy(want).cuda()
+    for col in (1, 4, d - 1):
+        fine[hit, ..., col] = w[hit][..., col].float()
+    check(dt, fine, lse, want, want_lse, v_max)
+    kx[where] = float("nan")
+    out, lse = run(kx, vx)
+    assert torch.isnan(out[hit].float()).all() and torch.isnan(lse[hit]).all()
+    check(dt, out[~hit], lse[~hit], want[~hit.cpu().numpy()], want_lse[~hit.cpu().numpy()], v_max)
+
+
+# ---------------------------------------------------------------------------
 # larger calls, against fp64 on the GPU
 # ---------------------------------------------------------------------------
 
