@@ -748,8 +748,8 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     -> (row_start int32 [n_seq + 1], slot int64 [tokens], pos int32 [tokens],
         used int64 [2]: pages taken from free_pages, new tokens left without a slot)
     """
-    env = _seq()
     dev = _index_of(cached, "cached")
+    env = _seq()
     _want(cached, "cached", env.i32, 1, dev)
     _want(fresh, "fresh", env.i32, 1, dev)
     _want(free_pages, "free_pages", env.i32, 1, dev)
@@ -786,8 +786,8 @@ def _pages(k_pages, v_pages, dtypes, index):
 def tod_page_write(k, v, slot, k_pages, v_pages, stream=None):
     """Write k, v [tokens, kv_heads, dim] into their slots (int64 [tokens], negative: none) of
     k_pages, v_pages [n_pages, kv_heads, page_rows, dim], in place."""
-    env = _seq()
     dev = _index_of(k, "k")
+    env = _seq()
     _want(k, "k", env.half, 3, dev, False)
     _want(v, "v", (k.dtype,), 3, dev, False)
     _want(slot, "slot", env.i64, 1, dev)
@@ -850,8 +850,8 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
     strides that are multiples of 8); row_start int32 [n_seq + 1].
     -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
     """
-    env = _seq()
     dev = _index_of(q, "q")
+    env = _seq()
     _want(q, "q", env.half, 3, dev, False)
     _want(k, "k", (q.dtype,), 3, dev, False)
     _want(v, "v", (q.dtype,), 3, dev, False)
@@ -882,8 +882,8 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
     where the caller knows it.
     -> out [tokens, heads, dim], and with return_lse the softmax's log sums fp32 [tokens, heads].
     """
-    env = _seq()
     dev = _index_of(q, "q")
+    env = _seq()
     _want(q, "q", env.half, 3, dev, False)
     n_pages, kv_heads, page_rows, dim = _pages(k_pages, v_pages, (q.dtype,), dev)
     _want(table, "table", env.i32, 2, dev)
