@@ -31,11 +31,32 @@ template <int DP>
 constexpr int token_loads() { return 2 * kTokenKeys * DP * 2 / 1024; }
 
 // Stages of a sequence that is the token kernel's, else 0.
-__device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
-  if (s >= a.n_seq) return 0;
-  const Seq q = seq_of<true>(a, s);
+__device__ __forceinline__ int32_t token_stages(const AttnArgs& a, const Seq& q) {
   if (q.n <= 0 || (int64_t)q.n * a.group.d > a.skip_rows) return 0;
   return (q.keys + kTokenKeys - 1) / kTokenKeys;
+}
+__device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
+  return s < a.n_seq ? token_stages(a, seq_of<true>(a, s)) : 0;
+}
+
+// Of `all` stages worker w of `grid` (a power of two) has those from share(w) on; where there are
+// fewer stages than workers, one each.
+__device__ __forceinline__ int64_t share(int64_t w, int64_t all, uint32_t grid) {
+  return all < grid ? w : (all * w) >> (31 - __builtin_clz(grid));
+}
+
+// The worker that has stage x: from an estimate (below 2^53 exact to one) and its neighbours.
+__device__ __forceinline__ int64_t worker_of(int64_t x, int64_t all, uint32_t grid) {
+  if (all < grid) return x;
+  int64_t w = (int64_t)((double)x * grid / (double)all);
+  while (w > 0 && share(w, all, grid) > x) --w;
+  while (w + 1 < grid && share(w + 1, all, grid) <= x) ++w;
+  return w;
+}
+
+// n / d for n >= 0, d > 0, in 32 bits where they fit.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
+  return n <= 0xffffffffLL && d <= 0xffffffffLL ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
 // Inclusive prefix sum over the lanes.
@@ -63,43 +84,31 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   __shared__ __align__(16) uint16_t lds[kRing * 2 * kStage];
   const int lane = threadIdx.x, col = lane & 31, h = lane >> 5;
 
-  // Rows past the last sequence, where no tile kernel follows.
-  if (a.token_tail) {
-    const int32_t words = a.heads * a.dim / 8;
-    for (int32_t t = start_of(a, a.n_seq) + (int32_t)blockIdx.x; t < a.tokens;
-         t += (int32_t)gridDim.x) {
-      for (int32_t i = lane; i < words; i += 64)
-        ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
-      if (a.lse)
-        for (int32_t i = lane; i < a.heads; i += 64) a.lse[(int64_t)t * a.heads + i] = -INFINITY;
-    }
-  }
-
-  // The line of stages: lane l sums the sequences of its own segment.
+  // The line of stages: lane l sums the sequences of its own segment (of one, where there are no
+  // more than lanes: then it holds what that sequence is).
   const int32_t seg = (a.n_seq + 63) / 64, s0 = lane * seg;
-  int64_t mine = 0;
-  for (int32_t i = 0; i < seg; ++i) mine += token_stages(a, s0 + i);
+  const Seq own = s0 < a.n_seq ? seq_of<true>(a, s0) : Seq{0, 0, 0, 0};
+  int64_t mine = token_stages(a, own);
+  for (int32_t i = 1; i < seg; ++i) mine += token_stages(a, s0 + i);
   const int64_t incl = lane_prefix(mine);
-  const int64_t total = __shfl(incl, 63, 64);  // of one head
-  const int64_t all = total * a.kv_heads;
-  const int64_t workers = min((int64_t)gridDim.x, all);
+  const int64_t all = __shfl(incl, 63, 64) * a.kv_heads;
   if (blockIdx.x == 0) {  // for the join
     int64_t before = incl - mine;
     for (int32_t i = 0; i < seg && s0 + i < a.n_seq; ++i) {
       a.token_line[s0 + i] = before;
-      before += token_stages(a, s0 + i);
+      before += i == 0 ? token_stages(a, own) : token_stages(a, s0 + i);
     }
     if (lane == 63) a.token_line[a.n_seq] = incl;
   }
-  if ((int64_t)blockIdx.x >= workers) return;
-  int64_t at = all * (int64_t)blockIdx.x / workers;
-  const int64_t end = all * ((int64_t)blockIdx.x + 1) / workers;
+  // This worker's share of it.
+  int64_t at = share(blockIdx.x, all, gridDim.x), end = share(blockIdx.x + 1, all, gridDim.x);
+  if (end > all) at = end = all;
 
   // The sequence that holds stage `at`: its segment, then 64 sequences a step.
-  int32_t s;
-  int64_t off;  // of `at` in the sequence's stages of all heads
-  {
-    const int64_t target = at / a.kv_heads;
+  int32_t s = 0;
+  int64_t off = 0;  // of `at` in the sequence's stages of all heads
+  if (at < end) {
+    const int64_t target = quotient(at, a.kv_heads);
     const int L = __popcll(__ballot(incl - mine <= target)) - 1;
     int64_t before = __shfl(incl - mine, L, 64);
     int32_t first = L * seg;
@@ -123,14 +132,19 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
 
   const uint32_t base = mt::lds_off(lds);
   for (bool opening = true; at < end; opening = false) {
-    const Seq sq = seq_of<true>(a, s);
-    const int32_t stages = token_stages(a, s);
+    Seq sq;
+    if (seg == 1)
+      sq = {__builtin_amdgcn_readlane(own.start, s), __builtin_amdgcn_readlane(own.n, s),
+            __builtin_amdgcn_readlane(own.keys, s), __builtin_amdgcn_readlane(own.shift, s)};
+    else
+      sq = seq_of<true>(a, s);
+    const int32_t stages = token_stages(a, sq);
     if (stages == 0) {  // another kernel's, or idle
       ++s;
       off = 0;
       continue;
     }
-    const uint32_t head = (uint32_t)(off / stages);
+    const uint32_t head = (uint32_t)quotient(off, stages);
     const int32_t jb = (int32_t)(off - (int64_t)head * stages);
     const int32_t je = (int32_t)min((int64_t)stages, jb + (end - at));
 
@@ -258,44 +272,53 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
       off = 0;
     }
   }
+
+  // Rows past the last sequence, where no tile kernel takes them.
+  if (a.token_tail) {
+    const int32_t words = a.heads * a.dim / 8;
+    for (int32_t t = start_of(a, a.n_seq) + (int32_t)blockIdx.x; t < a.tokens;
+         t += (int32_t)gridDim.x) {
+      for (int32_t i = lane; i < words; i += 64)
+        ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
+      if (a.lse)
+        for (int32_t i = lane; i < a.heads; i += 64) a.lse[(int64_t)t * a.heads + i] = -INFINITY;
+    }
+  }
 }
 
-// Joins the pieces of a (sequence, key / value head) pair, one wave a row.
+// Joins the pieces of a (sequence, key / value head) pair, a wave a row at a time.
 template <typename ET, int DP>
-__global__ void __launch_bounds__(64) token_join_kernel(AttnArgs a, int32_t grid) {
-  uint32_t b = blockIdx.x;
-  const int32_t r = (int32_t)(b % (uint32_t)a.skip_rows);
-  b /= (uint32_t)a.skip_rows;
-  const uint32_t head = b % (uint32_t)a.kv_heads;
-  const int32_t s = (int32_t)(b / (uint32_t)a.kv_heads);
+__global__ void __launch_bounds__(512) token_join_kernel(AttnArgs a, uint32_t grid) {
+  const uint32_t s = div_by(blockIdx.x, a.heads_div), head = blockIdx.x - s * a.heads_div.d;
   const int64_t before = a.token_line[s], after = a.token_line[s + 1];
   const int64_t all = a.token_line[a.n_seq] * a.kv_heads, stages = after - before;
-  const Seq sq = seq_of<true>(a, s);
-  if (stages == 0 || r >= sq.n * (int32_t)a.group.d) return;
-  const int64_t workers = min((int64_t)grid, all);
-  const int64_t lo = before * a.kv_heads + head * stages, hi = lo + stages;
-  // Worker w has the stages from floor(w all / workers) on.
-  const int64_t w0 = ((lo + 1) * workers - 1) / all, w1 = (hi * workers - 1) / all;
+  const Seq sq = seq_of<true>(a, (int32_t)s);
+  if (stages == 0) return;
+  const int64_t lo = before * a.kv_heads + head * stages;
+  const int64_t w0 = worker_of(lo, all, grid), w1 = worker_of(lo + stages - 1, all, grid);
   if (w0 == w1) return;
-  const int32_t tok = (int32_t)div_by((uint32_t)r, a.group);
-  const int32_t qh = (int32_t)head * (int32_t)a.group.d + r - tok * (int32_t)a.group.d;
-  const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
   // The first worker's piece is its last one if the pair begins within its share; the others
   // begin with theirs.
-  const bool within = w0 * all / workers < lo;
-  const int64_t row0 = (2 * w0 + within) * a.skip_rows + r, row1 = 2 * (w0 + 1) * a.skip_rows + r;
-  join_row<ET, DP>(a.token_stat, a.token_o, row0, row1, 2 * (int64_t)a.skip_rows,
-                   (int32_t)(w1 - w0 + 1), (ET*)a.out + orow * a.dim,
-                   a.lse ? a.lse + orow : nullptr, a.dim);
+  const bool within = share(w0, all, grid) < lo;
+  const int32_t rows = sq.n * (int32_t)a.group.d;
+  for (int32_t r = (int32_t)(threadIdx.x >> 6); r < rows; r += (int32_t)(blockDim.x >> 6)) {
+    const int32_t tok = (int32_t)div_by((uint32_t)r, a.group);
+    const int32_t qh = (int32_t)head * (int32_t)a.group.d + r - tok * (int32_t)a.group.d;
+    const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
+    join_row<ET, DP>(a.token_stat, a.token_o, (2 * w0 + within) * a.skip_rows + r,
+                     2 * (w0 + 1) * a.skip_rows + r, 2 * (int64_t)a.skip_rows,
+                     (int32_t)(w1 - w0 + 1), (ET*)a.out + orow * a.dim,
+                     a.lse ? a.lse + orow : nullptr, a.dim);
+  }
 }
 
 template <typename ET, int DP>
 hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
   const int64_t grid = token_workers(a.dim);
+  const unsigned waves = a.skip_rows < 8 ? (unsigned)a.skip_rows : 8u;
   hipLaunchKernelGGL((token_kernel<ET, DP>), dim3((unsigned)grid), dim3(64), 0, s, a);
-  hipLaunchKernelGGL((token_join_kernel<ET, DP>),
-                     dim3((unsigned)((int64_t)a.n_seq * a.kv_heads * a.skip_rows)), dim3(64), 0, s,
-                     a, (int32_t)grid);
+  hipLaunchKernelGGL((token_join_kernel<ET, DP>), dim3((unsigned)((int64_t)a.n_seq * a.kv_heads)),
+                     dim3(64 * waves), 0, s, a, (uint32_t)grid);
   return hipGetLastError();
 }
 

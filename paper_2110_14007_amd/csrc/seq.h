@@ -76,7 +76,7 @@ struct AttnArgs {
 
 // Packed rows that the token kernel takes: a product's 32 columns.
 constexpr int kTokenMaxRows = 32;
-// Its workers: four waves on each of 256 compute units with 32 KiB of LDS buffers each, two with
+// Its workers, a power of two: four waves on each of 256 compute units with 32 KiB of LDS buffers each, two with
 // 64 KiB for more than 128 elements.  (Reads of 1.5 GiB by such waves alone: 6.1 TB/s with four
 // a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
 inline int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
