@@ -7,7 +7,7 @@
 // split over several workgroups and a second kernel joins their results.
 #pragma once
 
-#include "attn.h"
+#include "attn_token.h"
 
 namespace tod {
 namespace attn {
@@ -83,6 +83,22 @@ __device__ __forceinline__ const void* uniform(const void* p) {
   return (const void*)(uintptr_t)(((uint64_t)hi << 32) | lo);
 }
 
+// Token workers that share a workgroup's LDS in a tile kernel's launch.
+template <int DP>
+constexpr int tile_workers() { return 2 * kRing * kKeys * DP * 2 / token_lds<DP>(); }
+
+// The kernel's arguments, read anew: a branch that takes them this way leaves the scalar registers
+// of the other one alone.
+__device__ __forceinline__ AttnArgs own_args() {
+  typedef const __attribute__((address_space(4))) uint64_t* words;
+  words p = (words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  struct { uint64_t w[sizeof(AttnArgs) / 8]; } v;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(AttnArgs) / 8); ++i) v.w[i] = p[i];
+  return __builtin_bit_cast(AttnArgs, v);
+}
+
 template <typename ET, int DP, bool PAGED>
 __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3) tile_kernel(AttnArgs a) {
   using V8 = typename Frag<ET>::V;
@@ -95,6 +111,16 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3) t
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // The last workgroups, if any, are the token workers': they read the memory while the tiles
+  // that are left compute.
+  if constexpr (PAGED) {
+    if (blockIdx.x >= a.tile_groups) {
+      if (wave < tile_workers<DP>())
+        token_work<ET, DP>(own_args(), (blockIdx.x - a.tile_groups) * tile_workers<DP>() + wave,
+                           lds + wave * (token_lds<DP>() / 2));
+      return;
+    }
+  }
   const uint32_t b = div_by(blockIdx.x, a.parts_div), part = blockIdx.x - b * a.parts_div.d;
   const uint32_t at = div_by(b, a.heads_div), head = b - at * a.heads_div.d;
   Tile t;
@@ -403,8 +429,8 @@ hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
         (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kern, dim3((unsigned)(slots * a.kv_heads * a.tile_parts)), dim3(64 * kWaves),
-                     bytes, s, a);
+  const int64_t tokens = PAGED && a.skip_rows ? token_workers(DP) / tile_workers<DP>() : 0;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.tile_groups + tokens)), dim3(64 * kWaves), bytes, s, a);
   if (a.tile_parts > 1)
     hipLaunchKernelGGL((tile_join_kernel<ET, DP, PAGED>),
                        dim3((unsigned)(slots * a.kv_heads * (kRows / 16))), dim3(256), 0, s, a);

@@ -22,13 +22,16 @@ namespace tod {
 namespace attn {
 
 constexpr int kTokenKeys = 32;  // keys of a stage
-constexpr int kTokenRows = kTokenMaxRows;
 
 // Buffers of a wave's ring, and loads of a stage.
 template <int DP>
 constexpr int token_ring() { return DP == 64 ? 4 : 2; }
 template <int DP>
 constexpr int token_loads() { return 2 * kTokenKeys * DP * 2 / 1024; }
+
+// Bytes of the ring.
+template <int DP>
+constexpr int token_lds() { return token_ring<DP>() * 2 * kTokenKeys * DP * 2; }
 
 // Stages of a sequence that is the token kernel's, else 0.
 __device__ __forceinline__ int32_t token_stages(const AttnArgs& a, const Seq& q) {
@@ -41,12 +44,12 @@ __device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
 
 // Of `all` stages worker w of `grid` (a power of two) has those from share(w) on; where there are
 // fewer stages than workers, one each.
-__device__ __forceinline__ int64_t share(int64_t w, int64_t all, uint32_t grid) {
-  return all < grid ? w : (all * w) >> (31 - __builtin_clz(grid));
+__device__ __forceinline__ int64_t share(int64_t w, int64_t all, const uint32_t grid) {
+  return all < grid ? w : (all * w) / grid;
 }
 
 // The worker that has stage x: from an estimate (below 2^53 exact to one) and its neighbours.
-__device__ __forceinline__ int64_t worker_of(int64_t x, int64_t all, uint32_t grid) {
+__device__ __forceinline__ int64_t worker_of(int64_t x, int64_t all, const uint32_t grid) {
   if (all < grid) return x;
   int64_t w = (int64_t)((double)x * grid / (double)all);
   while (w > 0 && share(w, all, grid) > x) --w;
@@ -75,14 +78,16 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// A worker: a wave, with the LDS of its ring.
 template <typename ET, int DP>
-__global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
+__device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t worker,
+                                           uint16_t* const lds) {
+  constexpr uint32_t grid = (uint32_t)token_workers(DP);
   using V8 = typename Frag<ET>::V;
   using St = Stager<ET, DP, true, true>;
   constexpr int kStage = kTokenKeys * DP;  // elements of a K or V stage
   constexpr int kRing = token_ring<DP>(), kLoads = token_loads<DP>(), DB = DP / 32;
-  __shared__ __align__(16) uint16_t lds[kRing * 2 * kStage];
-  const int lane = threadIdx.x, col = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
 
   // The line of stages: lane l sums the sequences of its own segment (of one, where there are no
   // more than lanes: then it holds what that sequence is).
@@ -92,7 +97,7 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   for (int32_t i = 1; i < seg; ++i) mine += token_stages(a, s0 + i);
   const int64_t incl = lane_prefix(mine);
   const int64_t all = __shfl(incl, 63, 64) * a.kv_heads;
-  if (blockIdx.x == 0) {  // for the join
+  if (worker == 0) {  // for the join
     int64_t before = incl - mine;
     for (int32_t i = 0; i < seg && s0 + i < a.n_seq; ++i) {
       a.token_line[s0 + i] = before;
@@ -101,7 +106,7 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
     if (lane == 63) a.token_line[a.n_seq] = incl;
   }
   // This worker's share of it.
-  int64_t at = share(blockIdx.x, all, gridDim.x), end = share(blockIdx.x + 1, all, gridDim.x);
+  int64_t at = share(worker, all, grid), end = share(worker + 1, all, grid);
   if (end > all) at = end = all;
 
   // The sequence that holds stage `at`: its segment, then 64 sequences a step.
@@ -254,7 +259,7 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
         restore_nonfinite<ET, DP, true>(st, (ET*)a.out, 0, sq, 0, cleared, sq.keys);
     } else {
       // At most two of a worker's pieces are not whole: its first and its last.
-      const int64_t row0 = (2 * (int64_t)blockIdx.x + !opening) * a.skip_rows;
+      const int64_t row0 = (2 * (int64_t)worker + !opening) * a.skip_rows;
       if (col < rows) {
         store_part<DP>(o, a.token_o + (row0 + col) * DP, h);
         if (h == 0) a.token_stat[row0 + col] = {mref, sum};
@@ -276,8 +281,8 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   // Rows past the last sequence, where no tile kernel takes them.
   if (a.token_tail) {
     const int32_t words = a.heads * a.dim / 8;
-    for (int32_t t = start_of(a, a.n_seq) + (int32_t)blockIdx.x; t < a.tokens;
-         t += (int32_t)gridDim.x) {
+    for (int32_t t = start_of(a, a.n_seq) + (int32_t)worker; t < a.tokens;
+         t += (int32_t)grid) {
       for (int32_t i = lane; i < words; i += 64)
         ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
       if (a.lse)
@@ -286,9 +291,16 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   }
 }
 
+template <typename ET, int DP>
+__global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
+  __shared__ __align__(16) uint16_t lds[token_lds<DP>() / 2];
+  token_work<ET, DP>(a, blockIdx.x, lds);
+}
+
 // Joins the pieces of a (sequence, key / value head) pair, a wave a row at a time.
 template <typename ET, int DP>
-__global__ void __launch_bounds__(512) token_join_kernel(AttnArgs a, uint32_t grid) {
+__global__ void __launch_bounds__(512) token_join_kernel(AttnArgs a) {
+  constexpr uint32_t grid = (uint32_t)token_workers(DP);
   const uint32_t s = div_by(blockIdx.x, a.heads_div), head = blockIdx.x - s * a.heads_div.d;
   const int64_t before = a.token_line[s], after = a.token_line[s + 1];
   const int64_t all = a.token_line[a.n_seq] * a.kv_heads, stages = after - before;
@@ -314,11 +326,15 @@ __global__ void __launch_bounds__(512) token_join_kernel(AttnArgs a, uint32_t gr
 
 template <typename ET, int DP>
 hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
-  const int64_t grid = token_workers(a.dim);
+  hipLaunchKernelGGL((token_kernel<ET, DP>), dim3((unsigned)token_workers(DP)), dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename ET, int DP>
+hipError_t launch_token_join(const AttnArgs& a, hipStream_t s) {
   const unsigned waves = a.skip_rows < 8 ? (unsigned)a.skip_rows : 8u;
-  hipLaunchKernelGGL((token_kernel<ET, DP>), dim3((unsigned)grid), dim3(64), 0, s, a);
   hipLaunchKernelGGL((token_join_kernel<ET, DP>), dim3((unsigned)((int64_t)a.n_seq * a.kv_heads)),
-                     dim3(64 * waves), 0, s, a, (uint32_t)grid);
+                     dim3(64 * waves), 0, s, a);
   return hipGetLastError();
 }
 

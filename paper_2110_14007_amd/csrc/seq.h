@@ -68,6 +68,7 @@ struct AttnArgs {
   // Splits of a tile's keys.
   int32_t tile_slots;   // of a key / value head
   int32_t tile_parts;   // most splits of a tile
+  uint32_t tile_groups;  // workgroups: slots, heads, splits
   FastDiv parts_div, heads_div;  // by tile_parts and kv_heads
   int32_t part_keys;    // fewest keys of a split
   float2* tile_stat;    // [tiles of all heads, parts, rows]
@@ -79,7 +80,7 @@ constexpr int kTokenMaxRows = 32;
 // Its workers, a power of two: four waves on each of 256 compute units with 32 KiB of LDS buffers each, two with
 // 64 KiB for more than 128 elements.  (Reads of 1.5 GiB by such waves alone: 6.1 TB/s with four
 // a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
-inline int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
+constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
@@ -87,6 +88,8 @@ hipError_t launch_attn_tile_f16(const AttnArgs& a, bool paged, hipStream_t s);
 hipError_t launch_attn_tile_bf16(const AttnArgs& a, bool paged, hipStream_t s);
 hipError_t launch_attn_token_f16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_bf16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_token_join_f16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_token_join_bf16(const AttnArgs& a, hipStream_t s);
 
 // Records a call's error for tod_last_error (never throws) and returns it.
 tod_status set_error(tod_status s, const char* msg) noexcept;

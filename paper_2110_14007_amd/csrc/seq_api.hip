@@ -161,6 +161,7 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool pag
   a->token_o = (float*)(base + p.token_o);
   a->tile_slots = (int32_t)p.tile_slots;
   a->tile_parts = p.tile_parts;
+  a->tile_groups = (uint32_t)(p.tile_slots * o.kv_heads * p.tile_parts);
   a->parts_div = tod::fast_div((uint32_t)p.tile_parts);
   a->part_keys = kPartKeys;
   a->tile_stat = (float2*)(base + p.tile_stat);
@@ -168,9 +169,13 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool pag
   const hipStream_t s = (hipStream_t)stream;
   const bool half = o.precision == TOD_PREC_FP16;
   hipError_t e = hipSuccess;
-  if (p.tile) e = half ? tod::launch_attn_tile_f16(*a, paged, s) : tod::launch_attn_tile_bf16(*a, paged, s);
-  if (e == hipSuccess && p.skip_rows)
+  // The tile kernel's launch holds the token workers too.
+  if (p.tile)
+    e = half ? tod::launch_attn_tile_f16(*a, paged, s) : tod::launch_attn_tile_bf16(*a, paged, s);
+  else
     e = half ? tod::launch_attn_token_f16(*a, s) : tod::launch_attn_token_bf16(*a, s);
+  if (e == hipSuccess && p.skip_rows)
+    e = half ? tod::launch_attn_token_join_f16(*a, s) : tod::launch_attn_token_join_bf16(*a, s);
   return launched(e, where);
 }
 
