@@ -105,8 +105,9 @@ __device__ __forceinline__ float other_half(float v) {
 // Stage layout: row-major, DP elements a row, with its 16-byte pieces c at
 // c ^ swizzle(row).  K is read by 32 rows at one piece: over any 16 rows that
 // differ modulo 16 the pieces fall on different banks.  V is read by the
-// transposing read, four rows of 32 bytes at a time.  (Reads measured at
-// 320-345 bytes / ns a compute unit for K and 195 for V; with no swizzle 38 and 151.)
+// transposing read, four rows of 32 bytes at a time.  (Reads measured at 343
+// bytes / ns a compute unit for K and 244 for V, whose reads reach 248 at best;
+// with no swizzle 38 and 151.)
 template <int DP>
 __device__ __forceinline__ int swizzle_k(int row) {
   return DP == 64 ? (row >> 1) & 7 : row & 15;
@@ -131,7 +132,7 @@ __device__ __forceinline__ void dma16_once(const void* g, uint32_t lds) {
 // Over pages, lane l holds entry `first` + l of the sequence's table, so that
 // a stage (64 keys at most) finds its rows without a load from memory unless
 // it leaves those 64 pages.
-template <typename ET, int DP, bool PAGED, bool ONCE = false>
+template <typename ET, int DP, bool PAGED>
 struct Stager {
   static constexpr int kPieces = DP / 8;       // 16-byte pieces of a row
   static constexpr int kRowsLoad = 64 / kPieces;  // rows that one load of the wave moves
@@ -195,30 +196,21 @@ struct Stager {
     mt::dma16(src, to + 2u * (uint32_t)(r0 * DP));
   }
 
-  // Rows r0 .. r0 + kRowsLoad - 1 of a stage whose K begins at LDS address k and V at v; at: place().
+  // Rows r0 .. r0 + kRowsLoad - 1 of a stage over pages whose K begins at LDS address k and V at v,
+  // read by no other wave; at: place().
   __device__ __forceinline__ void load(uint32_t at, int r0, uint32_t k, uint32_t v) const {
     const int lane = threadIdx.x & 63;
     const int r = r0 + lane / kPieces, pc = lane % kPieces;
     const uint32_t row = (uint32_t)__shfl((int)at, r, 64);
     const int ck = 8 * (pc ^ swizzle_k<DP>(r)), cv = 8 * (pc ^ swizzle_v<DP>(r));
-    const ET *kp, *vp;
-    if constexpr (PAGED) {
-      kp = (const ET*)a.k + (int64_t)row * a.dim;
-      vp = (const ET*)a.v + (int64_t)row * a.dim;
-    } else {
-      kp = (const ET*)a.k + (int64_t)row * a.k_row + (int64_t)head * a.k_head;
-      vp = (const ET*)a.v + (int64_t)row * a.v_row + (int64_t)head * a.v_head;
-    }
+    static_assert(PAGED, "rows of a cache");
+    const ET* const kp = (const ET*)a.k + (int64_t)row * a.dim;
+    const ET* const vp = (const ET*)a.v + (int64_t)row * a.dim;
     const bool ok = row != ~0u;
     const void* const ks = ok && ck < a.dim ? (const void*)(kp + ck) : &kZeros;
     const void* const vs = ok && cv < a.dim ? (const void*)(vp + cv) : &kZeros;
-    if constexpr (ONCE) {
-      dma16_once(ks, k + 2u * (uint32_t)(r0 * DP));
-      dma16_once(vs, v + 2u * (uint32_t)(r0 * DP));
-    } else {
-      mt::dma16(ks, k + 2u * (uint32_t)(r0 * DP));
-      mt::dma16(vs, v + 2u * (uint32_t)(r0 * DP));
-    }
+    dma16_once(ks, k + 2u * (uint32_t)(r0 * DP));
+    dma16_once(vs, v + 2u * (uint32_t)(r0 * DP));
   }
 };
 
@@ -300,8 +292,9 @@ __device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int ste
 }
 
 // After the stores of a wave's 32 packed rows from m0 on: where a row sees values that are not
-// finite among the keys j0 .. j1 - 1, they are added to its output (the weights are positive).  step 0: rows of the output; else partial results
-// of the rows one after the other, step elements each.
+// finite among the keys j0 .. j1 - 1, they are added to its output (the weights are positive).
+// step 0: rows of the output; else partial results of the rows one after the other, step elements
+// each.
 template <typename ET, int DP, bool PAGED, typename OT, typename ST>
 __device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step, const Seq& s,
                                                   int32_t m0, int32_t j0, int32_t j1) {

@@ -217,7 +217,9 @@ __global__ void __launch_bounds__(256) page_write_kernel(PageWriteArgs a) {
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s) {
   const int64_t blocks = (a.tokens + kMapTokens - 1) / kMapTokens;
-  // One request a thread while one round takes them all: its chain of sums is the shortest.
+  // One request a thread while one round takes them all: its chain is the shortest (48 requests
+  // 4.2 us, eight a thread 7.0).  Beyond that eight, for fewer rounds (2,000 requests 10.7 us, one
+  // a thread 14.3).
   const auto kern = a.n_seq <= kMapThreads ? page_map_kernel<1> : page_map_kernel<8>;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kMapThreads), 0, s, a);
   return hipGetLastError();
