@@ -15,7 +15,7 @@
 // TFLOP/s of bf16, where an 8192^3 matrix product reaches 1,182.  32 rows a wave
 // leave room for two workgroups a compute unit, whose waves fill each other's
 // gaps; 64 rows a wave halve the LDS reads, but need all 512 registers and were
-// slower.  24 packed prompts of up to 2,500 tokens take 0.49 - 0.56 ms, 750 - 650
+// slower.  24 packed prompts of up to 2,500 tokens take 0.49 to 0.56 ms, 855 to 745
 // TFLOP/s: a third of a workgroup's time is its start and its stores there.
 #pragma once
 
