@@ -388,18 +388,25 @@ __device__ __forceinline__ void store_part(const f32x16 (&o)[DP / 32], float* p,
     }
 }
 
-// One wave joins `parts` partial results of a row: (m, sum) at stat[row], the DP columns of O at
-// o[row * DP], for row = row0, then row1, row1 + step, ...  Lane l takes columns DP / 64 l on.
-template <typename ET, int DP>
-__device__ __forceinline__ void join_row(const float2* stat, const float* o, int64_t row0,
-                                         int64_t row1, int64_t step, int32_t parts, ET* out,
-                                         float* lse, int32_t dim) {
+// A row's running maximum, sum and O: lane l holds columns DP / 64 l on.
+template <int DP>
+struct Joined {
+  float m, sum, acc[DP / 64];
+};
+
+// One wave joins the partial results i .. end - 1 of a row: (m, sum) at stat[row], the DP columns
+// of O at o[row * DP], where row is row0 for the first, then row1, row1 + step, ...
+template <int DP>
+__device__ __forceinline__ Joined<DP> join_parts(const float2* stat, const float* o, int64_t row0,
+                                                 int64_t row1, int64_t step, int32_t i,
+                                                 int32_t end) {
   constexpr int C = DP / 64;
   const int lane = threadIdx.x & 63;
-  auto row_of = [&](int32_t i) { return i == 0 ? row0 : row1 + (i - 1) * step; };
-  float m = kNoMax, sum = 0.0f, acc[C] = {};
-  for (int32_t i0 = 0; i0 < parts; i0 += 64) {  // 64 parts a turn, the statistics one a lane
-    const int32_t n = min(parts - i0, 64);
+  auto row_of = [&](int32_t k) { return k == 0 ? row0 : row1 + (k - 1) * step; };
+  Joined<DP> j = {kNoMax, 0.0f, {}};
+  auto& [m, sum, acc] = j;
+  for (int32_t i0 = i; i0 < end; i0 += 64) {  // 64 parts a turn, the statistics one a lane
+    const int32_t n = min(end - i0, 64);
     const float2 st = lane < n ? stat[row_of(i0 + lane)] : float2{kNoMax, 0.0f};
     float top = fmaxf(m, st.x);
 #pragma unroll
@@ -429,11 +436,19 @@ __device__ __forceinline__ void join_row(const float2* stat, const float* o, int
       }
     }
   }
-  const float inv = inverse(sum);
+  return j;
+}
+
+template <typename ET, int DP>
+__device__ __forceinline__ void store_joined(const Joined<DP>& j, ET* out, float* lse,
+                                             int32_t dim) {
+  constexpr int C = DP / 64;
+  const int lane = threadIdx.x & 63;
+  const float inv = inverse(j.sum);
 #pragma unroll
   for (int c = 0; c < C; ++c)
-    if (C * lane + c < dim) out[C * lane + c] = (ET)(acc[c] * inv);
-  if (lse && lane == 0) *lse = log_sum(m, sum);
+    if (C * lane + c < dim) out[C * lane + c] = (ET)(j.acc[c] * inv);
+  if (lse && lane == 0) *lse = log_sum(j.m, j.sum);
 }
 
 }  // namespace attn

@@ -427,8 +427,9 @@ __global__ void __launch_bounds__(256) tile_join_kernel(AttnArgs a) {
     const int32_t qh = (int32_t)head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
     const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
     const int64_t row = (int64_t)b * a.tile_parts * kRows + r;
-    join_row<ET, DP>(a.tile_stat, a.tile_o, row, row + kRows, kRows, t.parts,
-                     (ET*)a.out + orow * a.dim, a.lse ? a.lse + orow : nullptr, a.dim);
+    store_joined<ET, DP>(
+        join_parts<DP>(a.tile_stat, a.tile_o, row, row + kRows, kRows, 0, t.parts),
+        (ET*)a.out + orow * a.dim, a.lse ? a.lse + orow : nullptr, a.dim);
   }
 }
 

@@ -302,30 +302,58 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
   token_work<ET, DP>(a, blockIdx.x, lds);
 }
 
-// Joins the pieces of a (sequence, key / value head) pair, a wave a row at a time.
-template <typename ET, int DP>
-__global__ void __launch_bounds__(512) token_join_kernel(AttnArgs a) {
+// Joins the pieces of a (sequence, key / value head) pair.  ALL: a workgroup of kJoinWaves waves
+// takes one of its packed rows, and each wave an equal part of the row's pieces.  Otherwise it
+// takes all of the pair's rows, a wave a row at a time.
+constexpr int kJoinWaves = 8;
+template <typename ET, int DP, bool ALL>
+__global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a) {
   constexpr uint32_t grid = (uint32_t)token_workers(DP);
-  const uint32_t s = div_by(blockIdx.x, a.heads_div), head = blockIdx.x - s * a.heads_div.d;
+  const uint32_t row = ALL ? blockIdx.x % (uint32_t)a.skip_rows : 0;
+  const uint32_t pair = ALL ? blockIdx.x / (uint32_t)a.skip_rows : blockIdx.x;
+  const uint32_t s = div_by(pair, a.heads_div), head = pair - s * a.heads_div.d;
   const int64_t before = a.token_line[s], after = a.token_line[s + 1];
   const int64_t all = a.token_line[a.n_seq] * a.kv_heads, stages = after - before;
   const Seq sq = seq_of<true>(a, (int32_t)s);
-  if (stages == 0) return;
+  const int32_t rows = sq.n * (int32_t)a.group.d;
+  if (stages == 0 || (int32_t)row >= rows) return;
   const int64_t lo = before * a.kv_heads + head * stages;
   const int64_t w0 = worker_of(lo, all, grid), w1 = worker_of(lo + stages - 1, all, grid);
   if (w0 == w1) return;
   // The first worker's piece is its last one if the pair begins within its share; the others
   // begin with theirs.
   const bool within = share(w0, all, grid) < lo;
-  const int32_t rows = sq.n * (int32_t)a.group.d;
-  for (int32_t r = (int32_t)(threadIdx.x >> 6); r < rows; r += (int32_t)(blockDim.x >> 6)) {
+  const int32_t pieces = (int32_t)(w1 - w0 + 1);
+  auto join = [&](int32_t r, int32_t from, int32_t to) {
+    return join_parts<DP>(a.token_stat, a.token_o, (2 * w0 + within) * a.skip_rows + r,
+                          2 * (w0 + 1) * a.skip_rows + r, 2 * (int64_t)a.skip_rows, from, to);
+  };
+  auto store = [&](int32_t r, const Joined<DP>& j) {
     const int32_t tok = (int32_t)div_by((uint32_t)r, a.group);
     const int32_t qh = (int32_t)head * (int32_t)a.group.d + r - tok * (int32_t)a.group.d;
     const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
-    join_row<ET, DP>(a.token_stat, a.token_o, (2 * w0 + within) * a.skip_rows + r,
-                     2 * (w0 + 1) * a.skip_rows + r, 2 * (int64_t)a.skip_rows,
-                     (int32_t)(w1 - w0 + 1), (ET*)a.out + orow * a.dim,
-                     a.lse ? a.lse + orow : nullptr, a.dim);
+    store_joined<ET, DP>(j, (ET*)a.out + orow * a.dim, a.lse ? a.lse + orow : nullptr, a.dim);
+  };
+  const int wave = (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if constexpr (ALL) {
+    __shared__ Joined<DP> left[kJoinWaves][64];
+    Joined<DP> j = join((int32_t)row, pieces * wave / kJoinWaves, pieces * (wave + 1) / kJoinWaves);
+    left[wave][lane] = j;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int i = 1; i < kJoinWaves; ++i) {
+      const Joined<DP> k = left[i][lane];
+      const float top = fmaxf(j.m, k.m);
+      const float f = __builtin_amdgcn_exp2f(j.m - top), g = __builtin_amdgcn_exp2f(k.m - top);
+      j.m = top;
+      j.sum = j.sum * f + k.sum * g;
+#pragma unroll
+      for (int c = 0; c < DP / 64; ++c) j.acc[c] = j.acc[c] * f + k.acc[c] * g;
+    }
+    store((int32_t)row, j);
+  } else {
+    for (int32_t r = wave; r < rows; r += kJoinWaves) store(r, join(r, 0, pieces));
   }
 }
 
@@ -337,9 +365,17 @@ hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
 
 template <typename ET, int DP>
 hipError_t launch_token_join(const AttnArgs& a, hipStream_t s) {
-  const unsigned waves = a.skip_rows < 8 ? (unsigned)a.skip_rows : 8u;
-  hipLaunchKernelGGL((token_join_kernel<ET, DP>), dim3((unsigned)((int64_t)a.n_seq * a.kv_heads)),
-                     dim3(64 * waves), 0, s, a);
+  // A pair has some workers / pairs pieces; from 16 on a workgroup a row joins them sooner (2
+  // sequences of 20,000 to 32,000 tokens, 2 heads: the whole call 24 us, with a wave a row 50), and
+  // below that a wave a row (16 of 3,000 to 9,000, 8 heads: 75.6 us, with a workgroup a row 77.4).
+  const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
+  const unsigned rows = (unsigned)a.skip_rows;
+  if (16 * pairs <= token_workers(DP))
+    hipLaunchKernelGGL((token_join_kernel<ET, DP, true>), dim3((unsigned)pairs * rows),
+                       dim3(64 * kJoinWaves), 0, s, a);
+  else
+    hipLaunchKernelGGL((token_join_kernel<ET, DP, false>), dim3((unsigned)pairs),
+                       dim3(64 * (rows < kJoinWaves ? rows : kJoinWaves)), 0, s, a);
   return hipGetLastError();
 }
 
