@@ -216,17 +216,17 @@ struct Stager {
 
 // Query operand: elements 16 c + 8 h .. + 7 of row p, zero from dim on.  Every lane loads (from the
 // row's start where there is nothing): with a branch around each, the loads would run one by one.
-template <typename ET, int DP>
-__device__ __forceinline__ void load_query(typename Frag<ET>::V (&q)[DP / 16], const ET* p,
+template <typename ET, int W>
+__device__ __forceinline__ void load_query(typename Frag<ET>::V (&q)[W / 16], const ET* p,
                                            int32_t dim, int h) {
-  u32x4 w[DP / 16];
+  u32x4 w[W / 16];
 #pragma unroll
-  for (int c = 0; c < DP / 16; ++c) {
+  for (int c = 0; c < W / 16; ++c) {
     const int e = 16 * c + 8 * h;
     w[c] = *(const u32x4*)(p + (e < dim ? e : 0));
   }
 #pragma unroll
-  for (int c = 0; c < DP / 16; ++c) {
+  for (int c = 0; c < W / 16; ++c) {
     const bool in = 16 * c + 8 * h < dim;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[c][i] = in ? w[c][i] : 0u;
@@ -351,13 +351,13 @@ __device__ __forceinline__ float log_sum(float m, float sum) {
 // out: rows that lie at the lanes' element offsets `at` (below 0: no such row).  They pass through
 // the wave's own 32 x DP elements of LDS at `lds`, so that each store writes whole rows: from
 // the accumulators a lane could write 8 bytes at a time only.
-template <typename ET, int DP>
-__device__ __forceinline__ void store_rows(const f32x16 (&o)[DP / 32], float f, ET* out, int64_t at,
+template <typename ET, int DP, int W>
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[W / 32], float f, ET* out, int64_t at,
                                            int32_t dim, uint16_t* lds) {
   constexpr int kPieces = DP / 8, kRowsStore = 64 / kPieces;  // 16-byte pieces; rows of a store
   const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
+  for (int d = 0; d < W / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       uint2 w;
@@ -377,10 +377,10 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[DP / 32], float f, 
 }
 
 // The same, unscaled fp32, into a row of a split's partial result.
-template <int DP>
-__device__ __forceinline__ void store_part(const f32x16 (&o)[DP / 32], float* p, int h) {
+template <int W>
+__device__ __forceinline__ void store_part(const f32x16 (&o)[W / 32], float* p, int h) {
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
+  for (int d = 0; d < W / 32; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float4 w = {o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};

@@ -28,6 +28,7 @@ constexpr int kWaves = 4;
 constexpr int kRows = 32 * kWaves;  // rows of a workgroup
 constexpr int kKeys = 32;           // keys of a stage
 constexpr int kRing = 4;            // stages of K, and of V, in LDS
+constexpr uint32_t kNoLoad = ~0u;   // offset of a lane that loads nothing
 constexpr float kSlack = 8.0f;  // growth of the maximum (log2) that m may lag behind
 
 // What a workgroup works on.
@@ -111,7 +112,9 @@ __device__ __forceinline__ AttnArgs own_args() {
   return __builtin_bit_cast(AttnArgs, v);
 }
 
-template <typename ET, int DP, bool PAGED>
+// W: the elements of a row that the products take, of the DP that its stages have room for.  FULL:
+// the rows have DP elements.
+template <typename ET, int DP, int W, bool FULL, bool PAGED>
 __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     tile_kernel(AttnArgs a) {
   using V8 = typename Frag<ET>::V;
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   constexpr int kStage = kKeys * DP;         // elements of a stage
   constexpr int kRowsWave = kKeys / kWaves;  // rows of a stage that a wave loads
   constexpr int kLoads = kRowsWave / St::kRowsLoad;
-  constexpr int DB = DP / 32, KC = DP / 16;
+  constexpr int DB = W / 32, KC = W / 16;
   extern __shared__ __align__(16) uint16_t lds[];  // kRing K stages, then as many V stages
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
@@ -152,7 +155,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   const int32_t least = PAGED || a.causal ? min(t.shift + tok0, t.keys - 1) : t.keys - 1;
   const int32_t open = min(max((least + 1) / kKeys - jb, 0), count);
   V8 q[KC];
-  load_query<ET, DP>(q, (const ET*)a.q + (int64_t)(t.start + tok) * a.q_row + (int64_t)qh * a.q_head,
+  load_query<ET, W>(q, (const ET*)a.q + (int64_t)(t.start + tok) * a.q_row + (int64_t)qh * a.q_head,
                      a.dim, h);
 
   // Staging.
@@ -169,15 +172,20 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int row = wave * kRowsWave + i * St::kRowsLoad + r;
-      ko[i] = (uint32_t)(2 * (kr * r + 8 * (pc ^ swizzle_k<DP>(row))));
+      const int c = 8 * (pc ^ swizzle_k<DP>(row));
+      ko[i] = c < a.dim ? (uint32_t)(2 * (kr * r + c)) : kNoLoad;
     }
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i)
-      vo[i] = (uint32_t)(2 * (vr * r + 8 * (pc ^ swizzle_v<DP>(i * St::kRowsLoad + r))));
+    for (int i = 0; i < kTurns; ++i) {
+      const int c = 8 * (pc ^ swizzle_v<DP>(i * St::kRowsLoad + r));
+      vo[i] = c < a.dim ? (uint32_t)(2 * (vr * r + c)) : kNoLoad;
+    }
   }
   // Whole stages whose rows of a wave lie together move by a base of the wave and an offset of
-  // the lane that stays; the others (the last stage, small or odd pages, padded rows) one by one.
-  const bool plain = a.dim == DP && (!PAGED || a.page.d % kRowsWave == 0);
+  // the lane that stays; the others (the last stage, small or odd pages, strides for which those
+  // offsets would pass 32 bits) one by one.  Pieces from dim on are not loaded: the stages are
+  // cleared once.  (Of every load some lane has a piece, so that the loads in flight count the same.)
+  const bool plain = PAGED ? a.page.d % kRowsWave == 0 : max(a.k_row, a.v_row) < (1 << 27);
   const int32_t fast = plain ? __builtin_amdgcn_readfirstlane(t.seen / kKeys - jb) : 0;
   const int32_t first = __builtin_amdgcn_readfirstlane(jb * kKeys + wave * kRowsWave);
   const ET *kb, *vb;
@@ -196,18 +204,21 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     if constexpr (PAGED) row = i < fast ? st.row_of(first + i * kKeys) : ~0u;
     if (PAGED ? row != ~0u : i < fast) {
       const ET* p;
-      int64_t stride = DP;
+      int64_t stride = FULL ? DP : a.dim;
       if constexpr (PAGED) {
-        p = (const ET*)(isk ? a.k : a.v) + (int64_t)row * DP;
+        p = (const ET*)(isk ? a.k : a.v) + (int64_t)row * stride;
       } else {
         stride = isk ? a.k_row : a.v_row;
         p = isk ? kb : vb;
         (isk ? kb : vb) += kKeys * stride;
       }
 #pragma unroll
-      for (int l = 0; l < kLoads; ++l)
-        dma16_at(p + l * St::kRowsLoad * stride, isk ? ko[l] : vo[l % kTurns],
-                 base + buf + 2u * (uint32_t)(wave * kRowsWave * DP + l * St::kRowsLoad * DP));
+      for (int l = 0; l < kLoads; ++l) {
+        const uint32_t off = isk ? ko[l] : vo[l % kTurns];
+        if (FULL || off != kNoLoad)
+          dma16_at(p + l * St::kRowsLoad * stride, off,
+                   base + buf + 2u * (uint32_t)(wave * kRowsWave * DP + l * St::kRowsLoad * DP));
+      }
       return;
     }
     const uint32_t at = st.place((jb + i) * kKeys, kKeys);
@@ -226,8 +237,10 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   float mref = kNoMax, sum = 0.0f;
   float limit_raw = -INFINITY;  // a score above it makes m follow
   // P of the stage before the first is zero, and so must its values be.
-  for (int i = tid; i < kStage / 8; i += 64 * kWaves)
-    ((uint4*)(lds + (2 * kRing - 1) * kStage))[i] = uint4{0, 0, 0, 0};
+  for (int i = (FULL ? 2 * kRing - 1 : 0) * kStage / 8 + tid; i < 2 * kRing * kStage / 8;
+       i += 64 * kWaves)
+    ((uint4*)lds)[i] = uint4{0, 0, 0, 0};
+  if constexpr (!FULL) mt::stage_barrier();
 
   // LDS addresses of this lane's fragments in buffer 0; the rest is a constant offset.
   typedef __attribute__((address_space(3))) const char* ldsp;
@@ -394,7 +407,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   const bool mine = t.row0 + 32 * wave + col < t.rows;
   if (t.parts > 1) {
     const int64_t row = ((int64_t)b * a.tile_parts + part) * kRows + 32 * wave + col;
-    if (mine) store_part<DP>(o, a.tile_o + row * DP, h);
+    if (mine) store_part<W>(o, a.tile_o + row * DP, h);
     if (mine && h == 0) a.tile_stat[row] = {mref, sum};
     if (cleared)
       restore_nonfinite<ET, DP, PAGED>(st, a.tile_o + (row - col) * DP, DP, t, t.row0 + 32 * wave,
@@ -404,7 +417,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
   if (mine && a.lse && h == 0) a.lse[orow] = log_sum(mref, sum);
   mt::stage_barrier();  // the other waves' reads of the stages are done
-  store_rows<ET, DP>(o, inverse(sum), (ET*)a.out, mine ? orow * a.dim : -1, a.dim,
+  store_rows<ET, DP, W>(o, inverse(sum), (ET*)a.out, mine ? orow * a.dim : -1, a.dim,
                      lds + wave * 32 * DP);
   if (cleared)
     restore_nonfinite<ET, DP, PAGED>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, (jb + open) * kKeys,
@@ -433,11 +446,11 @@ __global__ void __launch_bounds__(256) tile_join_kernel(AttnArgs a) {
   }
 }
 
-template <typename ET, int DP, bool PAGED>
+template <typename ET, int DP, int W, bool FULL, bool PAGED>
 hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
   const int64_t slots = a.tile_slots;
   constexpr unsigned bytes = 2 * kRing * kKeys * DP * 2;  // K and V, 16 bits
-  const auto kern = tile_kernel<ET, DP, PAGED>;
+  const auto kern = tile_kernel<ET, DP, W, FULL, PAGED>;
   if constexpr (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
@@ -449,6 +462,17 @@ hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((tile_join_kernel<ET, DP, PAGED>),
                        dim3((unsigned)(slots * a.kv_heads * (kRows / 16))), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+template <typename ET, bool PAGED>
+hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
+  if (a.dim < 64) return launch_tile<ET, 64, 64, false, PAGED>(a, s);
+  if (a.dim == 64) return launch_tile<ET, 64, 64, true, PAGED>(a, s);
+  if (a.dim <= 96) return launch_tile<ET, 128, 96, false, PAGED>(a, s);
+  if (a.dim < 128) return launch_tile<ET, 128, 128, false, PAGED>(a, s);
+  if (a.dim == 128) return launch_tile<ET, 128, 128, true, PAGED>(a, s);
+  if (a.dim < 256) return launch_tile<ET, 256, 256, false, PAGED>(a, s);
+  return launch_tile<ET, 256, 256, true, PAGED>(a, s);
 }
 
 }  // namespace attn

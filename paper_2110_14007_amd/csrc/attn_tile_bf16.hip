@@ -4,12 +4,7 @@
 namespace tod {
 
 hipError_t launch_attn_tile_bf16(const AttnArgs& a, bool paged, hipStream_t s) {
-  using ET = __bf16;
-  if (a.dim <= 64)
-    return paged ? attn::launch_tile<ET, 64, true>(a, s) : attn::launch_tile<ET, 64, false>(a, s);
-  if (a.dim <= 128)
-    return paged ? attn::launch_tile<ET, 128, true>(a, s) : attn::launch_tile<ET, 128, false>(a, s);
-  return paged ? attn::launch_tile<ET, 256, true>(a, s) : attn::launch_tile<ET, 256, false>(a, s);
+  return paged ? attn::launch_tile<__bf16, true>(a, s) : attn::launch_tile<__bf16, false>(a, s);
 }
 
 }  // namespace tod

@@ -259,7 +259,7 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
     if (jb == 0 && je == stages) {
       const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
       if (a.lse && h == 0 && col < rows) a.lse[orow] = log_sum(mref, sum);
-      store_rows<ET, DP>(o, inverse(sum), (ET*)a.out, col < rows ? orow * a.dim : -1, a.dim, lds);
+      store_rows<ET, DP, DP>(o, inverse(sum), (ET*)a.out, col < rows ? orow * a.dim : -1, a.dim, lds);
       if (cleared >= 0)
         restore_nonfinite<ET, DP, true>(st, (ET*)a.out, 0, sq, 0, cleared, sq.keys);
     } else {
