@@ -484,7 +484,8 @@ tod_status tod_loci(const float* x, int64_t n, int64_t d, const double* radii, i
  *
  * Packed sequences: n_seq sequences share `tokens` rows; sequence s holds the
  * rows row_start[s] .. row_start[s + 1] - 1 (int32 [n_seq + 1], ascending from
- * 0; entries are cut to [0, tokens]).  Sequences may be empty.
+ * 0; entries are cut to [0, tokens]).  Sequences may be empty.  Where starts do
+ * not ascend, the call's output rows are unspecified and may stay unwritten.
  *
  * Paged cache: k_pages and v_pages are [n_pages, kv_heads, page_rows, dim],
  * contiguous.  table[n_seq, table_cols] (int32) holds a sequence's pages in

@@ -42,7 +42,9 @@ struct Tile : Seq {
 // R_s = row_start[s] G, owns the slots from floor(R_s / kRows) + s on: at
 // least as many as it has tiles, whatever the lengths, and the last slot is
 // known on the host without them.  The search takes 64 candidates a step (one
-// a lane).  Sequences of at most skip_rows rows are the token kernel's.
+// a lane).  Starts that do not ascend can make it end at a sequence whose slots
+// begin past b: that slot is left empty, as its rows would lie outside the call.
+// Sequences of at most skip_rows rows are the token kernel's.
 template <bool PAGED>
 __device__ __forceinline__ bool find_tile(const AttnArgs& a, int32_t b, Tile* t) {
   const int lane = threadIdx.x & 63;
@@ -70,7 +72,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int32_t b, Tile* t)
   const int32_t row0 = (b - slot_of(lo, first)) * kRows;
   t->seq = lo;
   t->rows = t->n * (int32_t)a.group.d;
-  if (row0 >= t->rows || (lo < a.n_seq && t->rows <= a.skip_rows)) return false;
+  if (row0 < 0 || row0 >= t->rows || (lo < a.n_seq && t->rows <= a.skip_rows)) return false;
   t->row0 = row0;
   const int32_t last = (int32_t)div_by((uint32_t)min(t->row0 + kRows - 1, t->rows - 1), a.group);
   t->seen = PAGED || a.causal ? min(t->shift + last + 1, t->keys) : t->keys;
