@@ -54,7 +54,8 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   const int tid = threadIdx.x;
   const int32_t tokens = (int32_t)a.tokens;
   const int32_t t0 = (int32_t)blockIdx.x * kMapTokens;
-  const int32_t t1 = min(t0 + kMapTokens, tokens);
+  const int32_t count = min(kMapTokens, tokens - t0);  // (t0 + kMapTokens may be 2^31)
+  const int32_t t1 = t0 + count;
   const int32_t room = (int32_t)(a.cols * a.page.d);  // positions that the table holds
   const bool first = blockIdx.x == 0;
   for (int i = tid; i < kMapTokens; i += kMapThreads) mark[i] = -1;
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   for (int k = 0; k < kPlaces; ++k) {
     const int i = tid + k * kMapThreads;
     const int place = mark[i];
-    const bool live = place >= 0 && t0 + i < min((int64_t)t1, sum_fresh);
+    const bool live = place >= 0 && i < count && t0 + i < sum_fresh;
     const int64_t r = live ? who[place] : 0;
     const int32_t c = max(a.cached[r], 0);
     const int64_t at = (int64_t)c + (live ? t0 + i - start_of[place] : 0);
@@ -186,8 +187,8 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   }
 #pragma unroll
   for (int k = 0; k < kPlaces; ++k) {
-    const int32_t t = t0 + tid + k * kMapThreads;
-    if (t >= t1) break;
+    const int32_t i = tid + k * kMapThreads, t = t0 + i;
+    if (i >= count) break;
     if (entry[k]) *entry[k] = page[k];
     a.slot[t] = page[k] >= 0 ? (int64_t)page[k] * a.page.d + in[k] : -1;
     if (a.pos) a.pos[t] = pos[k];
