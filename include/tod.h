@@ -562,6 +562,10 @@ void tod_default_attn(tod_attn* attn, int32_t heads, int32_t kv_heads, int32_t d
  *   q [tokens, heads, dim], k, v [tokens, kv_heads, dim]; 16-byte aligned
  *   out [tokens, heads, dim] contiguous; lse_out [tokens, heads] fp32, nullable
  * A row that sees no key, such as one past row_start[n_seq], gets 0 and -inf.
+ * Keys and values that a row does not see do not reach it, whatever they hold.
+ * Where it sees values that are infinite or NaN, their sum is its output in
+ * that column (every weight counts as positive, however small); a NaN score
+ * makes the row NaN.
  * Workspace: tod_attn_workspace_size(attn, tokens, n_seq, tokens) bytes, 256-byte
  * aligned (0: invalid sizes); nothing in it lasts beyond the call.
  */

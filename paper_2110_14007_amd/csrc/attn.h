@@ -291,49 +291,84 @@ __device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int ste
     if ((vs[i] & 0x7fff) >= kInf) vs[i] = 0;
 }
 
+// Whether v is neither an infinity nor a NaN.  (These files are compiled as if none met a NaN: the
+// compiler must not know that the bits are a float's, or it leaves the NaN out of the test.)
+__device__ __forceinline__ bool finite(float v) {
+  uint32_t u = __float_as_uint(v);
+  asm("" : "+v"(u));
+  return (u & 0x7f800000u) != 0x7f800000u;
+}
+
+// Whether O of some of the wave's 32 rows, whose sums of weights are `sum`, met values that are not
+// finite: the sum of magnitudes shows one, at an addition an element.
+template <int N>
+__device__ __forceinline__ bool met_nonfinite(const f32x16 (&o)[N], float sum) {
+  float all = 0.0f;
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) all += fabsf(o[d][r]);
+  return __ballot(!finite(all) && finite(sum)) != 0;
+}
+
 // After the stores of a wave's 32 packed rows from m0 on: where a row sees values that are not
-// finite among the keys j0 .. j1 - 1, they are added to its output (the weights are positive).
-// step 0: rows of the output; else partial results of the rows one after the other, step elements
-// each.
+// finite among the keys j0 .. j1 - 1, its output is their sum, since all weights are positive.
+// (The products do not say so: a value may have been cleared, or met a weight or a half of one that
+// was rounded to 0.)  Rows whose weights are NaN, so that `sum` is, stay NaN.  step 0: rows of the
+// output; else partial results of the rows one after the other, step elements each.
 template <typename ET, int DP, bool PAGED, typename OT, typename ST>
 __device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step, const Seq& s,
-                                                  int32_t m0, int32_t j0, int32_t j1) {
+                                                  int32_t m0, int32_t j0, int32_t j1, float sum) {
   const AttnArgs& a = st.a;
   const int lane = threadIdx.x & 63;
   constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
+  const uint64_t sound = __ballot(finite(sum));
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores that this one follows
 #pragma unroll 1
-  for (int32_t r = 0; r < 32; ++r) {
-    const int32_t m = m0 + r;
-    if (m >= s.n * (int32_t)a.group.d) break;
-    const int32_t tok = (int32_t)div_by((uint32_t)m, a.group);
-    const int32_t end = min(min(s.shift + tok + 1, s.keys), j1);
-    const int64_t row = (int64_t)(s.start + tok) * a.heads +
-                        (int64_t)st.head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
-    OT* const to = step ? out + (int64_t)r * step : out + row * a.dim;
+  for (int32_t e = lane; e < a.dim; e += 64) {
+    float total = 0.0f;
+    bool any = false;
+    int32_t j = j0;  // (each row sees at least the keys of the one before)
 #pragma unroll 1
-    for (int32_t e = lane; e < a.dim; e += 64) {
-      float sum = 0.0f;
-      bool any = false;
+    for (int32_t r = 0; r < 32; ++r) {
+      const int32_t m = m0 + r;
+      if (m >= s.n * (int32_t)a.group.d) break;
+      const int32_t tok = (int32_t)div_by((uint32_t)m, a.group);
+      const int32_t end = min(PAGED || a.causal ? min(s.shift + tok + 1, s.keys) : s.keys, j1);
+      constexpr int kAhead = 8;  // values in flight; the last again where there are fewer
 #pragma unroll 1
-      for (int32_t j = j0; j < end; ++j) {
-        const ET* p = (const ET*)a.v;
-        if constexpr (PAGED) {
-          const uint32_t pg = div_by((uint32_t)j, a.page);
-          const int32_t id = a.table[(int64_t)st.seq * a.cols + pg];
-          if (id < 0 || id >= a.n_pages) continue;
-          p += (((int64_t)id * a.kv_heads + st.head) * a.page.d + (j - (int32_t)(pg * a.page.d))) *
-               a.dim;
-        } else {
-          p += (int64_t)(s.start + j) * a.v_row + (int64_t)st.head * a.v_head;
+      for (; j < end; j += min(end - j, kAhead)) {
+        uint16_t u[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int32_t key = min(j + k, end - 1);
+          const ET* p = (const ET*)a.v;
+          if constexpr (PAGED) {
+            const uint32_t pg = div_by((uint32_t)key, a.page);
+            const int32_t id = a.table[(int64_t)st.seq * a.cols + pg];
+            const bool none = id < 0 || id >= a.n_pages;  // zeros
+            p += (((int64_t)id * a.kv_heads + st.head) * a.page.d +
+                  (key - (int32_t)(pg * a.page.d))) * a.dim;
+            const uint16_t* const from = (const uint16_t*)p + e;
+            u[k] = *(none ? (const uint16_t*)&kZeros : from);
+          } else {
+            p += (int64_t)(s.start + key) * a.v_row + (int64_t)st.head * a.v_head;
+            u[k] = ((const uint16_t*)p)[e];
+          }
         }
-        const uint16_t u = ((const uint16_t*)p)[e];
-        if ((u & 0x7fff) >= kInf) {
-          any = true;
-          sum += (float)__builtin_bit_cast(ET, u);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          if ((u[k] & 0x7fff) >= kInf) {
+            any = true;
+            total += (float)__builtin_bit_cast(ET, u[k]);
+          }
         }
       }
-      if (any) to[e] = (OT)((float)to[e] + sum);  // (still NaN where the weights are)
+      if (any && (sound >> r & 1)) {
+        const int64_t row = (int64_t)(s.start + tok) * a.heads +
+                            (int64_t)st.head * (int32_t)a.group.d + m - tok * (int32_t)a.group.d;
+        (step ? out + (int64_t)r * step : out + row * a.dim)[e] = (OT)total;
+      }
     }
   }
 }
@@ -388,6 +423,9 @@ __device__ __forceinline__ void store_part(const f32x16 (&o)[W / 32], float* p, 
     }
 }
 
+// A part of O by its weight.  What is not finite stays what it is, also where the weight is 0.
+__device__ __forceinline__ float weighted(float v, float w) { return finite(v) ? v * w : v; }
+
 // A row's running maximum, sum and O: lane l holds columns DP / 64 l on.
 template <int DP>
 struct Joined {
@@ -418,7 +456,7 @@ __device__ __forceinline__ Joined<DP> join_parts(const float2* stat, const float
     for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d, 64);
     sum = sum * keep + part;
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] *= keep;
+    for (int c = 0; c < C; ++c) acc[c] = weighted(acc[c], keep);
     constexpr int kAhead = 8;  // parts in flight
     for (int32_t i = 0; i < n; i += kAhead) {
       float v[kAhead][C];
@@ -432,7 +470,7 @@ __device__ __forceinline__ Joined<DP> join_parts(const float2* stat, const float
       for (int k = 0; k < kAhead; ++k) {  // a part past the last has weight 0 (i + k < 64)
         const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i + k));
 #pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] += i + k < n ? v[k][c] * w : 0.0f;
+        for (int c = 0; c < C; ++c) acc[c] += i + k < n ? weighted(v[k][c], w) : 0.0f;
       }
     }
   }

@@ -350,7 +350,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   constexpr int kS = 2 * kStage;  // bytes of a stage
   // Values that some rows of the tile do not see meet their zero weights in the second product,
   // which is no zero where a value is not finite.  Those values are cleared in their stage (of
-  // index i), and what they make of the rows that do see them is restored at the end.
+  // index i), and what they make of the rows that do see them is restored at the end, as it is for
+  // values that all rows see.
   bool cleared = false;
   auto clear = [&](int32_t i) __attribute__((always_inline)) {
     if (!(PAGED || a.causal)) return;
@@ -406,14 +407,15 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
                         __builtin_bit_cast(V8, count % 2 ? pa[c] : pb[c]), o[d]);
   }
   sum += other_half(sum);
+  const bool restore = cleared || met_nonfinite(o, sum);
   const bool mine = t.row0 + 32 * wave + col < t.rows;
   if (t.parts > 1) {
     const int64_t row = ((int64_t)b * a.tile_parts + part) * kRows + 32 * wave + col;
     if (mine) store_part<W>(o, a.tile_o + row * DP, h);
     if (mine && h == 0) a.tile_stat[row] = {mref, sum};
-    if (cleared)
+    if (restore)
       restore_nonfinite<ET, DP, PAGED>(st, a.tile_o + (row - col) * DP, DP, t, t.row0 + 32 * wave,
-                                       (jb + open) * kKeys, (jb + count) * kKeys);
+                                       jb * kKeys, (jb + count) * kKeys, sum);
     return;
   }
   const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
@@ -421,9 +423,9 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   mt::stage_barrier();  // the other waves' reads of the stages are done
   store_rows<ET, DP, W>(o, inverse(sum), (ET*)a.out, mine ? orow * a.dim : -1, a.dim,
                      lds + wave * 32 * DP);
-  if (cleared)
-    restore_nonfinite<ET, DP, PAGED>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, (jb + open) * kKeys,
-                                     (jb + count) * kKeys);
+  if (restore)
+    restore_nonfinite<ET, DP, PAGED>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, jb * kKeys,
+                                     (jb + count) * kKeys, sum);
 }
 
 // Joins the splits of a tile, one wave a row.

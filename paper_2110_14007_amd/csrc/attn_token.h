@@ -190,7 +190,7 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     float mref = kNoMax, sum = 0.0f;
-    int32_t cleared = -1;  // from here on values that are not finite were taken for 0
+    bool cleared = false;  // values that are not finite were taken for 0
 
     for (int32_t j = jb; j < je; ++j) {
       if (j + kRing <= je)
@@ -230,7 +230,7 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
       // A value that is not finite must not meet the zero weight of a row that does not see it.
       if (j0 + kTokenKeys - 1 > wlo && rows > (int32_t)a.group.d && holds_nonfinite<ET, DP>(vs)) {
         clear_nonfinite<ET, DP>(lds + 2 * kStage * ((j - jb) % kRing) + kStage, 0, 64);
-        if (cleared < 0) cleared = j0;
+        cleared = true;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -255,13 +255,13 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
       }
     }
     sum += other_half(sum);
+    const bool restore = cleared || met_nonfinite(o, sum);
 
     if (jb == 0 && je == stages) {
       const int64_t orow = (int64_t)(sq.start + tok) * a.heads + qh;
       if (a.lse && h == 0 && col < rows) a.lse[orow] = log_sum(mref, sum);
       store_rows<ET, DP, DP>(o, inverse(sum), (ET*)a.out, col < rows ? orow * a.dim : -1, a.dim, lds);
-      if (cleared >= 0)
-        restore_nonfinite<ET, DP, true>(st, (ET*)a.out, 0, sq, 0, cleared, sq.keys);
+      if (restore) restore_nonfinite<ET, DP, true>(st, (ET*)a.out, 0, sq, 0, 0, sq.keys, sum);
     } else {
       // At most two of a worker's pieces are not whole: its first and its last.
       const int64_t row0 = (2 * (int64_t)worker + !opening) * a.skip_rows;
@@ -269,9 +269,9 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
         store_part<DP>(o, a.token_o + (row0 + col) * DP, h);
         if (h == 0) a.token_stat[row0 + col] = {mref, sum};
       }
-      if (cleared >= 0)
-        restore_nonfinite<ET, DP, true>(st, a.token_o + row0 * DP, DP, sq, 0, cleared,
-                                        je * kTokenKeys);
+      if (restore)
+        restore_nonfinite<ET, DP, true>(st, a.token_o + row0 * DP, DP, sq, 0, jb * kTokenKeys,
+                                        je * kTokenKeys, sum);
     }
     // Its stores and LDS reads are done before the next pair's loads are counted.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -349,7 +349,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a)
       j.m = top;
       j.sum = j.sum * f + k.sum * g;
 #pragma unroll
-      for (int c = 0; c < DP / 64; ++c) j.acc[c] = j.acc[c] * f + k.acc[c] * g;
+      for (int c = 0; c < DP / 64; ++c)
+        j.acc[c] = weighted(j.acc[c], f) + weighted(k.acc[c], g);
     }
     store((int32_t)row, j);
   } else {
