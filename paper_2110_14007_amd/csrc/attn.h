@@ -22,7 +22,8 @@
 // lanes read four rows of 16 columns, and lane i of them gets column i).
 //
 // Softmax.  In base 2: t = s scale log2(e), p = 2^(t - m) with m the running
-// maximum.  m, the sum and O are fp32, and the sum takes the unrounded p.
+// maximum.  m, the sum and O are fp32, and the sum takes the unrounded p, those of
+// a stage or of a few together.
 // Splits of the keys leave (m, sum, O) in the workspace, joined by 2^(m - max).
 #pragma once
 
@@ -290,6 +291,21 @@ __device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int ste
   for (int i = first + (threadIdx.x & 63); i < 32 * DP; i += step)
     if ((vs[i] & 0x7fff) >= kInf) vs[i] = 0;
 }
+
+// Adds the weights of a stage or of a few to a running sum, with what the additions before lost: a
+// long tail of keys whose weights are near 2^-24 of the sum would not move it otherwise.
+struct Sum {
+  float v = 0.0f, lost = 0.0f;
+  __device__ __forceinline__ void add(float part) {
+    const float x = part - lost, next = v + x;
+    lost = (next - v) - x;
+    v = next;
+  }
+  __device__ __forceinline__ void scale(float f) {
+    v *= f;
+    lost *= f;
+  }
+};
 
 // Whether v is neither an infinity nor a NaN.  (These files are compiled as if none met a NaN: the
 // compiler must not know that the bits are a float's, or it leaves the NaN out of the test.)

@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-  float mref = kNoMax, sum = 0.0f;
+  float mref = kNoMax, few = 0.0f;  // few: weights of up to four stages, on their way to acc
+  Sum acc;
   float limit_raw = -INFINITY;  // a score above it makes m follow
   // P of the stage before the first is zero, and so must its values be.
   for (int i = (FULL ? 2 * kRing - 1 : 0) * kStage / 8 + tid; i < 2 * kRing * kStage / 8;
@@ -314,7 +315,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
           const float f = __builtin_amdgcn_exp2f(mref - next);
           mref = next;
           limit_raw = (next + kSlack) * a.unscale;
-          sum *= f;
+          acc.scale(f);
+          few *= f;
 #pragma unroll
           for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -338,8 +340,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
           // half again as many MFMAs as the tile has.
           const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e], a.scale, -mref));
           const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e + 1], a.scale, -mref));
-          sum += x0;
-          sum += x1;
+          few += x0;
+          few += x1;
           pn[e / 4][e % 4] = pack2<ET>(x0, x1);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -395,7 +397,10 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     turn(j + 2, 2, sa, sb, pb, pa);
     if (j + 3 >= count) break;
     turn(j + 3, 3, sb, sa, pa, pb);
+    acc.add(few);
+    few = 0.0f;
   }
+  acc.add(few);
   if (count > 0) {
     if (count > open) clear(count - 1);
     const int at = (count - 1) % kRing * kS;
@@ -406,7 +411,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
         o[d] = mfma<ET>(vfrag(at + 16 * c * DP * 2, d),
                         __builtin_bit_cast(V8, count % 2 ? pa[c] : pb[c]), o[d]);
   }
-  sum += other_half(sum);
+  const float sum = acc.v + other_half(acc.v);
   const bool restore = cleared || met_nonfinite(o, sum);
   const bool mine = t.row0 + 32 * wave + col < t.rows;
   if (t.parts > 1) {

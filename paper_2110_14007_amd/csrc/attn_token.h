@@ -189,7 +189,8 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-    float mref = kNoMax, sum = 0.0f;
+    float mref = kNoMax;
+    Sum acc;
     bool cleared = false;  // values that are not finite were taken for 0
 
     for (int32_t j = jb; j < je; ++j) {
@@ -216,17 +217,19 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
         const float next = grow ? top : mref;
         const float f = __builtin_amdgcn_exp2f(mref - next);
         mref = next;
-        sum *= f;
+        acc.scale(f);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[d][r] *= f;
       }
+      float part = 0.0f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -mref));
-        sum += x[r];
+        part += x[r];
       }
+      acc.add(part);
       // A value that is not finite must not meet the zero weight of a row that does not see it.
       if (j0 + kTokenKeys - 1 > wlo && rows > (int32_t)a.group.d && holds_nonfinite<ET, DP>(vs)) {
         clear_nonfinite<ET, DP>(lds + 2 * kStage * ((j - jb) % kRing) + kStage, 0, 64);
@@ -254,7 +257,7 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
         stage(j + kRing);
       }
     }
-    sum += other_half(sum);
+    const float sum = acc.v + other_half(acc.v);
     const bool restore = cleared || met_nonfinite(o, sum);
 
     if (jb == 0 && je == stages) {
