@@ -24,6 +24,10 @@
 // Softmax.  In base 2: t = s scale log2(e), p = 2^(t - m) with m the running
 // maximum.  m, the sum and O are fp32, and the sum takes the unrounded p, those of
 // a stage or of a few together.
+// The second product takes p in the input type.  fp16 ends at 2^-24, where a long cache may have
+// most of its weight (100,000 keys of p = 2^-24 beside one of 1 are 0.6% of the output), so that
+// for fp16 m is the running maximum less kBias: weights reach 2^kBias, and what is rounded away
+// of each is 2^-35 of the largest at most.
 // Splits of the keys leave (m, sum, O) in the workspace, joined by 2^(m - max).
 #pragma once
 
@@ -44,6 +48,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Before the first visible key: every finite score replaces it.
 constexpr float kNoMax = -3.0e38f;
 constexpr float kLn2 = 0.69314718055994531f;
+// How far below the running maximum m is taken (log2).
+template <typename ET>
+constexpr float kBias = std::is_same<ET, _Float16>::value ? 10.0f : 0.0f;
+// Where |t| is larger, the rounding of t itself takes up the room that is left to fp16's 2^16: there
+// m is the maximum as it is.
+constexpr float kFar = 1048576.0f;
 
 // A sequence of the call.  After the last one comes one without keys that
 // holds the rows past row_start[n_seq].

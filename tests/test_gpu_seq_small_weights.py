@@ -6,6 +6,14 @@ All other keys have the same score, gap below the key's, so that with N of them
 Log sums, derived: they are sums of fp32 weights in which no addition loses more than it must
 (additions of weights near 2^-24 to 1, one by one, would lose up to all of them: 8e-3 here), so that
 what is left are a few roundings of numbers up to 35: 35 2^-22 = 1e-5; allowed are 1e-4.
+
+Outputs, derived with u = 2^-11 for fp16 and 2^-8 for bf16 (half an ulp at the most): the output is
+rounded, u |out| or, below fp16's normal range, 2^-25.  With v0 = 0 the weights are rounded all
+alike, u |out|.  With v0 = v1 that hardly counts, but an accumulator that is near 1 from the start
+takes N / 16 additions of 2^-24 at most, N 2^-28 <= 2^-11.  Weights below fp16's normal range are
+rounded to a multiple of 2^-24; the kernels take them times 2^10 at least where the largest is 1, so
+that each is off by at most 2^-35 and the sum by N 2^-35.  fp32 scores of up to 24 are off by
+24 2^-23, the weights by that factor: 3e-6.  Together (2 u + 3e-6) |out| + 2^-25 + N 2^-35.
 """
 import math
 
@@ -27,6 +35,7 @@ CASES = {
     "prompt": dict(keys=100003, fresh=0, at=50000),
     "prompt_first": dict(keys=120000, fresh=0, at=0),
 }
+U = {"float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
 GAPS = [16.0, 17.4, 18.0, 24.0]
 
 
@@ -72,3 +81,19 @@ def test_log_sums(name, dtype, gap):
     want = torch.where(seen > CASES[name]["at"],
                        gap + torch.log1p((seen - 1) * math.exp(-gap)), torch.log(seen))
     assert float((lse - want).abs().max()) <= 1e-4
+
+
+@pytest.mark.parametrize("v0", [0.0, 1.0])
+@pytest.mark.parametrize("gap", GAPS)
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_outputs(name, dtype, gap, v0):
+    import torch
+    out, _, seen, gap = attend(name, dtype, gap, v0)
+    has = seen > CASES[name]["at"]  # the key is among those that the row sees
+    others = (seen - 1) * math.exp(-gap)
+    want = torch.where(has, (v0 + others) / (1 + others), 1.0)
+    off = (out - want).abs()
+    allowed = (2 * U[dtype] + 3e-6) * want + 2.0 ** -25 + torch.where(has, seen, 0.0) * 2.0 ** -35
+    worst = int((off - allowed).argmax())
+    assert (off <= allowed).all(), (worst, float(out[worst]), float(want[worst]))
