@@ -72,8 +72,8 @@ tod_status check_rows(const tod_attn& a, int64_t tokens, int64_t n_seq) {
   if (tokens <= 0 || n_seq <= 0) return invalid("tokens and n_seq must be positive");
   if (n_seq > kMaxCount / 2) return unsupported("more than 2^30 - 1 sequences");
   const int64_t group = a.heads / a.kv_heads;
-  // Grids are 32 bits: a head's tile slots are tokens * group / 128 + n_seq + 1, with at most 16
-  // splits or 8 workgroups of the join each, and the tokens' join has 32 rows a sequence and head.
+  // Rows and tile slots (tokens * group / 128 + n_seq + 1 a head) in 32 bits; make_plan() has the
+  // launches.
   if (tokens > kMaxCount / 2 / group ||
       tokens * group / 128 + n_seq + 1 > kMaxCount / 32 / a.kv_heads)
     return unsupported("too many rows for one call");
@@ -104,6 +104,7 @@ struct Plan {
   int32_t skip_rows, tile_parts;
   int64_t tile_slots;
   bool tile;  // some sequence may have more rows than the token kernel takes
+  bool fits;  // every launch has fewer than 2^32 threads
   size_t line, token_stat, token_o, tile_stat, tile_o, total;
 };
 
@@ -148,12 +149,19 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
       p.tile_o = take(slots * p.tile_parts * 128 * dp * 4);
     }
   }
+  // (Where tiles are split, their slots times splits are few, and so are the join's workgroups.
+  // The tokens' join has a workgroup of a wave a row, at most 8, for every pair.)
+  constexpr int64_t kThreads = 1LL << 32;
+  const int64_t join = 64 * (p.skip_rows < 8 ? p.skip_rows : 8);
+  p.fits = (!p.tile || (p.tile_slots * o.kv_heads * p.tile_parts + 1024) * 256 < kThreads) &&
+           n_seq * o.kv_heads * join < kThreads;
   p.total = at ? at : 256;
   return p;
 }
 
 tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool paged, void* ws,
                     size_t ws_bytes, void* stream, const char* where) {
+  if (!p.fits) return unsupported("too many rows for one call");
   if (!aligned(ws, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
   if (ws_bytes < p.total)
     return set_error(TOD_ERR_WORKSPACE, "workspace smaller than tod_attn_workspace_size()");
@@ -279,9 +287,10 @@ size_t tod_attn_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_s
   tod_attn o;
   if (check_attn(attn, &o) != TOD_OK || check_rows(o, tokens, n_seq) != TOD_OK || max_fresh <= 0)
     return 0;
-  const size_t paged = make_plan(o, tokens, n_seq, max_fresh, true).total;
-  const size_t prompt = make_plan(o, tokens, n_seq, max_fresh, false).total;
-  return paged > prompt ? paged : prompt;
+  const Plan paged = make_plan(o, tokens, n_seq, max_fresh, true);
+  const Plan prompt = make_plan(o, tokens, n_seq, max_fresh, false);
+  const size_t a = paged.fits ? paged.total : 0, b = prompt.fits ? prompt.total : 0;
+  return a > b ? a : b;
 }
 
 tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, const void* v,
