@@ -581,7 +581,8 @@ tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, c
  * single tokens, or both.  Sequence s has cached[s] tokens in the cache before
  * this step, and its rows of q are the tokens that follow, whose keys and
  * values have been written too: token i of them sees the positions
- * 0 .. cached[s] + i (at most table_cols * page_rows of them).  Formulas and outputs
+ * 0 .. cached[s] + i (at most table_cols * page_rows of them, which with the
+ * tokens and 64 stay below 2^31).  Formulas and outputs
  * as tod_attn_prompt; attn->causal must be 1.  An entry of the table that is
  * no page counts as a page of zeros.
  *   max_fresh  no sequence has more new tokens than this (tokens is always

@@ -13,6 +13,7 @@ using tod::set_error;
 
 constexpr int64_t kMaxCount = 0x7fffffffLL;
 constexpr int32_t kPartKeys = 512;  // fewest keys of a split of a tile
+constexpr int64_t kBeyond = 64;     // positions past a sequence's last that its last stages name
 
 tod_status invalid(const char* msg) { return set_error(TOD_ERR_INVALID_ARG, msg); }
 tod_status unsupported(const char* msg) { return set_error(TOD_ERR_UNSUPPORTED, msg); }
@@ -337,8 +338,8 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
   if ((st = check_pages(n_pages, page_rows, o.kv_heads)) != TOD_OK) return st;
   if (table_cols <= 0 || max_fresh <= 0)
     return invalid("table_cols and max_fresh must be positive");
-  if (table_cols > (kMaxCount - tokens) / page_rows)
-    return unsupported("more than 2^31 - 1 positions");
+  if (table_cols > (kMaxCount - kBeyond - tokens) / page_rows)
+    return unsupported("positions that do not fit into 32 bits");
   if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
     return invalid("tensors must be 16-byte aligned");
   if (!aligned(table, 4) || !aligned(row_start, 4) || !aligned(cached, 4) || !aligned(lse_out, 4))

@@ -68,3 +68,16 @@ def test_workspace_sizes_of_what_fits(tod):
     assert _size(tod, 64, 8, 9, 1 << 21, 1) == 0  # neither call takes it
     assert _size(tod, 64, 8, 9, 1 << 20, 1) > 0  # a prompt call does
     assert _size(tod, 1, 1, 1, 1 << 25, 1) > 0  # a paged call does
+
+
+# Positions are 32 bits, with room for the call's tokens and the 64 positions that the stage after
+# the last key names.
+@pytest.mark.parametrize("page,cols,tokens,status", [
+    (1, (1 << 31) - 2, 1, UNSUPPORTED), (1, (1 << 31) - 1 - 64, 1, UNSUPPORTED),
+    (1, (1 << 31) - 1 - 64 - 1, 1, WORKSPACE), (2, (1 << 30) - 33, 3, UNSUPPORTED),
+    (2, (1 << 30) - 35, 3, WORKSPACE), (65536, 32767, 1000, WORKSPACE),
+    (65536, 32767, 65536, UNSUPPORTED),
+])
+def test_paged_positions(tod, page, cols, tokens, status):
+    assert _paged(tod, 1, 1, tokens, 1, tokens, cols, page) == status
+    assert tod.last_error() != ""
