@@ -668,6 +668,8 @@ class _Seq:
         self.stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
         self.device = torch._C._cuda_getDevice
         self.guard = torch.cuda.device
+        self.on = torch.cuda.stream
+        self.current = torch.cuda.current_stream
 
 
 _seq_env = None
@@ -711,8 +713,23 @@ def _strides(x, name):
     return (row if tokens > 1 else 0), (head if heads > 1 else dim)
 
 
+def _new(like, shape, dtype, stream):
+    """An uninitialised tensor that the stream may write at once.
+
+    torch's allocator hands memory that was freed on a stream to that stream's next tensor, while
+    its work may still use it: the memory has to come from the stream that the call runs on.  The
+    caller reads it on the current one."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    env = _seq()
+    with env.on(stream):
+        out = like.new_empty(shape, dtype=dtype)
+    out.record_stream(env.current(like.device))
+    return out
+
+
 def _queue(where, fn, index, stream, tensors, *args):
-    """fn(*args, stream pointer, ...) on the stream; args holds None in the stream's place.
+    """fn(*args, stream pointer, ...) on the stream; args holds _STREAM in the stream's place.
 
     The work outlives the call, and torch's allocator gives freed memory to the stream that it
     was allocated on: with a stream of the caller's, every tensor is recorded as used there."""
@@ -761,7 +778,7 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     room = max(tokens, 0)
     # One allocation: used, slot (int64), then row_start and pos (int32).
     words = 2 * (2 + room)
-    buf = cached.new_empty((words + n + 1 + room,))
+    buf = _new(cached, (words + n + 1 + room,), env.i32[0], stream)
     longs = buf[:words].view(env.i64[0])
     used, slot = longs[:2], longs[2:]
     row_start, pos = buf[words:words + n + 1], buf[words + n + 1:]
@@ -819,13 +836,21 @@ def _attn(q, kv_heads, causal, scale, k=None, v=None):
 _ATTN_SIZE = ctypes.sizeof(tod_attn)
 
 
-def _attn_outputs(q, out, return_lse):
+def _attn_outputs(q, out, return_lse, stream):
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _new(q, q.shape, q.dtype, stream)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device \
             or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
-    return out, (q.new_empty(q.shape[:2], dtype=_seq().f32[0]) if return_lse else None)
+    return out, (_new(q, q.shape[:2], _seq().f32[0], stream) if return_lse else None)
+
+
+def _attn_ws(workspace, nbytes, device, stream):
+    """_ws() with a buffer that the stream may write at once (see _new)."""
+    if stream is None:
+        return _ws(workspace, nbytes, device)
+    with _seq().on(stream):
+        return _ws(workspace, nbytes, device)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -861,9 +886,9 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
     if k.shape != (tokens, kv_heads, dim) or v.shape != k.shape:
         raise ValueError("k and v must be [tokens, kv_heads, dim] with q's tokens and dim")
     a = _attn(q, kv_heads, causal, scale, k, v)
-    out, lse = _attn_outputs(q, out, return_lse)
-    buf, ws, ws_bytes = _ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens),
-                            q.device)
+    out, lse = _attn_outputs(q, out, return_lse, stream)
+    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens),
+                                 q.device, stream)
     _queue("tod_attn_prompt", _lib.tod_attn_prompt, dev, stream,
            (q, k, v, row_start, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens,
@@ -896,10 +921,10 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
     if cached.shape[0] != n or row_start.shape[0] != n + 1:
         raise ValueError("table, row_start and cached must describe the same sequences")
     a = _attn(q, kv_heads, True, scale)
-    out, lse = _attn_outputs(q, out, return_lse)
+    out, lse = _attn_outputs(q, out, return_lse, stream)
     fresh = tokens if max_fresh is None else int(max_fresh)
-    buf, ws, ws_bytes = _ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh),
-                            q.device)
+    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh),
+                                 q.device, stream)
     _queue("tod_attn_paged", _lib.tod_attn_paged, dev, stream,
            (q, k_pages, v_pages, table, row_start, cached, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
