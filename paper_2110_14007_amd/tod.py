@@ -275,11 +275,19 @@ def _dev_matrix(x, name):
 
 
 class Workspace:
-    """Reusable device workspace (torch uint8 buffer, grown on demand)."""
+    """Reusable device workspace (torch uint8 buffer, grown on demand).
+
+    The sequence operators return before their work is done, so that each stream has a buffer of its
+    own: calls on one stream follow each other in it, calls on two may run at once.  A graph replays
+    into the buffers that it was captured with; they stay as long as this object, which the program
+    keeps as long as the graph.  (The replays of one graph share them: one at a time, and not while
+    other calls run on the stream that it was captured on.)"""
 
     def __init__(self, device=None):
         self.buf = None
         self.device = device
+        self._queued = {}    # (device, stream) -> buffer of calls that do not wait
+        self._captured = []  # buffers that graphs hold the addresses of
 
     def get(self, nbytes: int, device):
         torch = _torch()
@@ -287,11 +295,24 @@ class Workspace:
             self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
         return self.buf
 
+    def get_queued(self, nbytes: int, device):
+        """The buffer of the current stream, for a call that does not wait."""
+        env = _seq()
+        key = device.index, env.stream(device.index)
+        buf = self._queued.get(key)
+        if buf is None or buf.numel() < nbytes:
+            buf = _torch().empty(max(nbytes, 256), dtype=env.u8, device=device)
+            self._queued[key] = buf
+        if env.capturing() and not any(b is buf for b in self._captured):
+            self._captured.append(buf)
+        return buf
+
 
 class FixedWorkspace:
     """A device workspace of a fixed size chosen by the caller.  The library
     plans its query blocks to fit it (automatic batching sized to memory);
-    a workspace below the fixed buffers plus one 32-row block is an error."""
+    a workspace below the fixed buffers plus one 32-row block is an error.
+    It is one buffer: sequence operators that use it run on one stream."""
 
     def __init__(self, nbytes: int, device="cuda:0"):
         torch = _torch()
@@ -663,6 +684,7 @@ class _Seq:
     def __init__(self):
         torch = _torch()
         self.f32, self.i32, self.i64 = (torch.float32,), (torch.int32,), (torch.int64,)
+        self.u8 = torch.uint8
         self.half = (torch.float16, torch.bfloat16)
         self.fp16 = torch.float16
         self.stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
@@ -670,6 +692,7 @@ class _Seq:
         self.guard = torch.cuda.device
         self.on = torch.cuda.stream
         self.current = torch.cuda.current_stream
+        self.capturing = torch.cuda.is_current_stream_capturing
 
 
 _seq_env = None
@@ -845,12 +868,18 @@ def _attn_outputs(q, out, return_lse, stream):
     return out, (_new(q, q.shape[:2], _seq().f32[0], stream) if return_lse else None)
 
 
-def _attn_ws(workspace, nbytes, device, stream):
-    """_ws() with a buffer that the stream may write at once (see _new)."""
-    if stream is None:
-        return _ws(workspace, nbytes, device)
-    with _seq().on(stream):
-        return _ws(workspace, nbytes, device)
+def _attn_ws(workspace, nbytes, like, stream):
+    """(buffer, pointer, size) of a workspace that the stream may write at once (see _new)."""
+    if workspace is None:
+        buf = _new(like, (max(nbytes, 256),), _seq().u8, stream)
+    else:
+        get = getattr(workspace, "get_queued", workspace.get)
+        if stream is None:
+            buf = get(nbytes, like.device)
+        else:
+            with _seq().on(stream):
+                buf = get(nbytes, like.device)
+    return buf, ctypes.c_void_p(buf.data_ptr()), ctypes.c_size_t(buf.numel())
 
 
 @functools.lru_cache(maxsize=1024)
@@ -887,8 +916,8 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
         raise ValueError("k and v must be [tokens, kv_heads, dim] with q's tokens and dim")
     a = _attn(q, kv_heads, causal, scale, k, v)
     out, lse = _attn_outputs(q, out, return_lse, stream)
-    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens),
-                                 q.device, stream)
+    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens), q,
+                                 stream)
     _queue("tod_attn_prompt", _lib.tod_attn_prompt, dev, stream,
            (q, k, v, row_start, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens,
@@ -923,8 +952,8 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
     a = _attn(q, kv_heads, True, scale)
     out, lse = _attn_outputs(q, out, return_lse, stream)
     fresh = tokens if max_fresh is None else int(max_fresh)
-    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh),
-                                 q.device, stream)
+    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh), q,
+                                 stream)
     _queue("tod_attn_paged", _lib.tod_attn_paged, dev, stream,
            (q, k_pages, v_pages, table, row_start, cached, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
