@@ -674,7 +674,7 @@ def tod_loci(x, radii, alpha: float = 0.5, n_min: int = 20, k_sigma: float = 3.0
 
 
 # ---------------------------------------------------------------------------
-# sequence operators: queued on the stream, not waited for
+# sequence operators: queued on the stream, not waited for; forward only
 # ---------------------------------------------------------------------------
 
 class _Seq:
@@ -693,6 +693,7 @@ class _Seq:
         self.on = torch.cuda.stream
         self.current = torch.cuda.current_stream
         self.capturing = torch.cuda.is_current_stream_capturing
+        self.gradients = torch.is_grad_enabled
 
 
 _seq_env = None
@@ -716,6 +717,9 @@ def _want(x, name, dtypes, dim, index, contiguous=True):
     try:
         if (x.get_device() == index and x.dtype in dtypes and x.dim() == dim
                 and (not contiguous or x.is_contiguous())):
+            if x.requires_grad and _seq().gradients():
+                raise ValueError("%s requires a gradient, which this operator does not pass on: "
+                                 "detach it or call under torch.no_grad()" % name)
             return
     except AttributeError:
         pass
@@ -865,6 +869,8 @@ def _attn_outputs(q, out, return_lse, stream):
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device \
             or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
+    else:
+        _want(out, "out", (q.dtype,), 3, q.get_device())
     return out, (_new(q, q.shape[:2], _seq().f32[0], stream) if return_lse else None)
 
 
