@@ -788,7 +788,8 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     """Pages and slots of every sequence's new tokens.
 
     cached, fresh: int32 [n_seq]; free_pages: int32 [n_free]; table: int32 [n_seq, cols],
-    updated in place; tokens: the number of new tokens (a larger number pads the outputs).
+    updated in place; tokens: the number of new tokens (a larger number pads the outputs; with 0 the
+    table stays as it is).
     -> (row_start int32 [n_seq + 1], slot int64 [tokens], pos int32 [tokens],
         used int64 [2]: pages taken from free_pages, new tokens left without a slot)
     """
@@ -802,6 +803,16 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     if fresh.shape[0] != n or cached.shape[0] != n:
         raise ValueError("cached, fresh and table must have one row per sequence")
     tokens = int(tokens)
+    if tokens == 0:
+        with env.on(stream):
+            used = fresh.new_zeros((2,), dtype=env.i64[0])
+            used[1] = fresh.clamp(min=0).sum()  # all of them are left out
+            row_start = fresh.new_zeros((n + 1,))
+        if stream is not None:  # (see _queue and _new)
+            fresh.record_stream(stream)
+            for t in (row_start, used):
+                t.record_stream(env.current(dev))
+        return row_start, used.new_empty((0,)), fresh.new_empty((0,)), used
     room = max(tokens, 0)
     # One allocation: used, slot (int64), then row_start and pos (int32).
     words = 2 * (2 + room)
@@ -840,6 +851,8 @@ def tod_page_write(k, v, slot, k_pages, v_pages, stream=None):
     if k.shape != (tokens, kv_heads, dim) or v.shape != k.shape:
         raise ValueError("k and v must be [%d, %d, %d] as slot and the pages are"
                          % (tokens, kv_heads, dim))
+    if tokens == 0:
+        return
     (kr, kh), (vr, vh) = _strides(k, "k"), _strides(v, "v")
     _queue("tod_page_write", _lib.tod_page_write, dev, stream, (k, v, slot, k_pages, v_pages),
            k.data_ptr(), v.data_ptr(), tokens, kv_heads, dim, kr, kh, vr, vh, slot.data_ptr(),
@@ -922,6 +935,8 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
         raise ValueError("k and v must be [tokens, kv_heads, dim] with q's tokens and dim")
     a = _attn(q, kv_heads, causal, scale, k, v)
     out, lse = _attn_outputs(q, out, return_lse, stream)
+    if tokens == 0:
+        return (out, lse) if return_lse else out
     buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens), q,
                                  stream)
     _queue("tod_attn_prompt", _lib.tod_attn_prompt, dev, stream,
@@ -957,6 +972,8 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
         raise ValueError("table, row_start and cached must describe the same sequences")
     a = _attn(q, kv_heads, True, scale)
     out, lse = _attn_outputs(q, out, return_lse, stream)
+    if tokens == 0:
+        return (out, lse) if return_lse else out
     fresh = tokens if max_fresh is None else int(max_fresh)
     buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh), q,
                                  stream)
