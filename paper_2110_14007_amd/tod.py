@@ -862,9 +862,11 @@ def tod_page_write(k, v, slot, k_pages, v_pages, stream=None):
 def _attn(q, kv_heads, causal, scale, k=None, v=None):
     _, heads, dim = q.shape
     if scale is None:
-        scale = 0.0
-    elif not scale > 0.0:
-        raise ValueError("scale must be positive")
+        scale = 0.0  # the library's default
+    else:
+        scale = ctypes.c_float(scale).value
+        if not scale > 0.0:
+            raise ValueError("scale must be positive, and in 32 bits too")
     kr = kh = vr = vh = 0
     if k is not None:
         (kr, kh), (vr, vh) = _strides(k, "k"), _strides(v, "v")
