@@ -525,8 +525,8 @@ tod_status tod_page_map(const int32_t* cached, const int32_t* fresh, int64_t n_s
  * moved unchanged).  k, v: [tokens, kv_heads, dim], elements of a row
  * contiguous; *_row and *_head are the strides of tokens and heads in elements,
  * multiples of 8 (0: contiguous).  A token whose slot is outside
- * [0, n_pages * page_rows) is left out; of tokens that share a slot, either
- * may end up in it.  dim is a multiple of 8; tensors are 16-byte aligned.
+ * [0, n_pages * page_rows) is left out; a slot that several tokens share ends
+ * up with pieces of any of them.  dim is a multiple of 8; tensors are 16-byte aligned.
  */
 tod_status tod_page_write(const void* k, const void* v, int64_t tokens, int32_t kv_heads,
                           int32_t dim, int64_t k_row, int64_t k_head, int64_t v_row,

@@ -791,7 +791,8 @@ def tod_page_map(cached, fresh, free_pages, table, page_rows: int, tokens: int, 
     updated in place; tokens: the number of new tokens (a larger number pads the outputs; with 0 the
     table stays as it is).
     -> (row_start int32 [n_seq + 1], slot int64 [tokens], pos int32 [tokens],
-        used int64 [2]: pages taken from free_pages, new tokens left without a slot)
+        used int64 [2]: pages needed, which free_pages gives as far as it goes, and new tokens left
+        without a slot)
     """
     dev = _index_of(cached, "cached")
     env = _seq()
