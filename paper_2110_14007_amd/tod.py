@@ -279,15 +279,14 @@ class Workspace:
 
     The sequence operators return before their work is done, so that each stream has a buffer of its
     own: calls on one stream follow each other in it, calls on two may run at once.  A graph replays
-    into the buffers that it was captured with; they stay as long as this object, which the program
-    keeps as long as the graph.  (The replays of one graph share them: one at a time, and not while
-    other calls run on the stream that it was captured on.)"""
+    into the buffer that it was captured with, so that one that grew stays too, as long as this
+    object, which the program keeps as long as the graph.  (Its replays share that buffer: one at a
+    time, and not while other calls run on the stream that it was captured on.)"""
 
     def __init__(self, device=None):
         self.buf = None
         self.device = device
-        self._queued = {}    # (device, stream) -> buffer of calls that do not wait
-        self._captured = []  # buffers that graphs hold the addresses of
+        self._queued = {}  # (device, stream) -> buffers of calls that do not wait, the last in use
 
     def get(self, nbytes: int, device):
         torch = _torch()
@@ -297,15 +296,16 @@ class Workspace:
 
     def get_queued(self, nbytes: int, device):
         """The buffer of the current stream, for a call that does not wait."""
-        env = _seq()
-        key = device.index, env.stream(device.index)
-        buf = self._queued.get(key)
-        if buf is None or buf.numel() < nbytes:
-            buf = _torch().empty(max(nbytes, 256), dtype=env.u8, device=device)
-            self._queued[key] = buf
-        if env.capturing() and not any(b is buf for b in self._captured):
-            self._captured.append(buf)
-        return buf
+        index = device.index
+        bufs = self._queued.get((index, _seq().stream(index)))
+        if bufs is None:
+            bufs = self._queued.setdefault((index, _seq().stream(index)), [])
+        elif bufs[-1].numel() >= nbytes:
+            return bufs[-1]
+        # At least twice as large as the last: all that are kept are no more than that again.
+        least = 2 * bufs[-1].numel() if bufs else 256
+        bufs.append(_torch().empty(max(nbytes, least), dtype=_seq().u8, device=device))
+        return bufs[-1]
 
 
 class FixedWorkspace:
@@ -692,7 +692,6 @@ class _Seq:
         self.guard = torch.cuda.device
         self.on = torch.cuda.stream
         self.current = torch.cuda.current_stream
-        self.capturing = torch.cuda.is_current_stream_capturing
         self.gradients = torch.is_grad_enabled
 
 
@@ -891,17 +890,14 @@ def _attn_outputs(q, out, return_lse, stream):
 
 
 def _attn_ws(workspace, nbytes, like, stream):
-    """(buffer, pointer, size) of a workspace that the stream may write at once (see _new)."""
+    """A workspace of nbytes at least that the stream may write at once (see _new)."""
     if workspace is None:
-        buf = _new(like, (max(nbytes, 256),), _seq().u8, stream)
-    else:
-        get = getattr(workspace, "get_queued", workspace.get)
-        if stream is None:
-            buf = get(nbytes, like.device)
-        else:
-            with _seq().on(stream):
-                buf = get(nbytes, like.device)
-    return buf, ctypes.c_void_p(buf.data_ptr()), ctypes.c_size_t(buf.numel())
+        return _new(like, (max(nbytes, 256),), _seq().u8, stream)
+    get = workspace.get_queued if isinstance(workspace, Workspace) else workspace.get
+    if stream is None:
+        return get(nbytes, like.device)
+    with _seq().on(stream):
+        return get(nbytes, like.device)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -940,12 +936,11 @@ def tod_attn_prompt(q, k, v, row_start, causal: bool = True, scale=None, workspa
     out, lse = _attn_outputs(q, out, return_lse, stream)
     if tokens == 0:
         return (out, lse) if return_lse else out
-    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens), q,
-                                 stream)
+    buf = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, tokens), q, stream)
     _queue("tod_attn_prompt", _lib.tod_attn_prompt, dev, stream,
            (q, k, v, row_start, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens,
-           row_start.data_ptr(), n, ws, ws_bytes, _STREAM, out.data_ptr(),
+           row_start.data_ptr(), n, buf.data_ptr(), buf.numel(), _STREAM, out.data_ptr(),
            lse.data_ptr() if return_lse else None)
     return (out, lse) if return_lse else out
 
@@ -978,13 +973,13 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
     if tokens == 0:
         return (out, lse) if return_lse else out
     fresh = tokens if max_fresh is None else int(max_fresh)
-    buf, ws, ws_bytes = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh), q,
-                                 stream)
+    buf = _attn_ws(workspace, _attn_room(heads, kv_heads, dim, tokens, n, fresh), q, stream)
     _queue("tod_attn_paged", _lib.tod_attn_paged, dev, stream,
            (q, k_pages, v_pages, table, row_start, cached, out, lse, buf),
            ctypes.byref(a), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), n_pages,
            page_rows, table.data_ptr(), cols, row_start.data_ptr(), cached.data_ptr(), n, tokens,
-           fresh, ws, ws_bytes, _STREAM, out.data_ptr(), lse.data_ptr() if return_lse else None)
+           fresh, buf.data_ptr(), buf.numel(), _STREAM, out.data_ptr(),
+           lse.data_ptr() if return_lse else None)
     return (out, lse) if return_lse else out
 
 
