@@ -449,8 +449,10 @@ __device__ __forceinline__ void store_part(const f32x16 (&o)[W / 32], float* p, 
     }
 }
 
-// A part of O by its weight.  What is not finite stays what it is, also where the weight is 0.
-__device__ __forceinline__ float weighted(float v, float w) { return finite(v) ? v * w : v; }
+// A part of O by its weight.  An infinity stays one, also where the weight is 0.
+__device__ __forceinline__ float weighted(float v, float w) {
+  return fabsf(v) == INFINITY ? v : v * w;
+}
 
 // A row's running maximum, sum and O: lane l holds columns DP / 64 l on.
 template <int DP>
