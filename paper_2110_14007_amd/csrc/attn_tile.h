@@ -11,11 +11,12 @@
 // Bound by the matrix and vector instructions that a SIMD's two waves issue: a
 // stage is 16 MFMAs (14.3 ns each from one SIMD), 16 exponentials a lane (4.6)
 // and some 60 other vector instructions (2.1), and the clock falls to 1.75 GHz
-// under them.  One prompt of 16,001 tokens, 32 heads of 128, takes 1.89 ms: 1,110
-// TFLOP/s of bf16, where an 8192^3 matrix product reaches 1,182.  32 rows a wave
+// under them.  One prompt of 16,001 tokens, 32 heads of 128, takes 1.91 to 2.03 ms on
+// three cards: 1,100 to 1,035 TFLOP/s of bf16, where an 8192^3 matrix product
+// reaches 1,182.  32 rows a wave
 // leave room for two workgroups a compute unit, whose waves fill each other's
 // gaps; 64 rows a wave halve the LDS reads, but need all 512 registers and were
-// slower.  24 packed prompts of up to 2,500 tokens take 0.49 to 0.56 ms, 855 to 745
+// slower.  24 packed prompts of up to 2,500 tokens take 0.49 to 0.60 ms, 850 to 700
 // TFLOP/s: a third of a workgroup's time is its start and its stores there.
 #pragma once
 

@@ -16,10 +16,10 @@
 // what the rounding lost: the weights then keep 16 bits, in fp16 down to 2^-19
 // of the largest (each is off by 2^-35 of it at most).
 //
-// Measured, with 8 heads of 128: 248 us for 3 caches of 120,000 to 131,071
-// tokens (6.2 TB/s, the rate of a plain read), 229 us for 96 of 100 to 6,000
-// (5.2 TB/s), 7.3 us for one of 900, where a worker has one stage and its start
-// counts; the join takes 5 us more.
+// Measured, with 8 heads of 128: 243 us for 3 caches of 120,000 to 131,071
+// tokens (6.3 TB/s, the rate of a plain read), 224 us for 96 of 100 to 6,000
+// (5.4 TB/s), 7.3 us for one of 900, where a worker has one stage and its start
+// counts; the join takes 5 to 8 us more.
 #pragma once
 
 #include "attn.h"

@@ -44,7 +44,7 @@ __device__ __forceinline__ T block_prefix(T v, T* total, int64_t* lds) {
 // token its request.  A token that opens a page writes the table's entry, so
 // long requests are spread over many threads.  A thread takes EACH neighbouring
 // requests of a round.  Bound by latency: launch, the lengths, two prefix sums.
-// 4.2 us for 48 requests of one token, 10.8 us for 2,000 with 54,900.
+// 4.3 us for 48 requests of one token, 10.8 us for 2,000 with 54,900.
 template <int EACH>
 __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   __shared__ int64_t sums[kMapThreads / 64];
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
 
 // One thread moves 16 bytes of a key row and of its value row.  Bound by the
 // bytes: 4 d a token and head in each direction.  48 tokens of 8 heads of 128
-// take 2.5 us (a launch), 20,011 of them 25 us (6.6 TB/s of both directions).
+// take 2.6 us (a launch), 20,011 of them 25 us (6.6 TB/s of both directions).
 __global__ void __launch_bounds__(256) page_write_kernel(PageWriteArgs a) {
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
   const uint32_t t = div_by(i, a.per_token);

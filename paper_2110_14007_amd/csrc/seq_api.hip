@@ -133,12 +133,12 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
   p.tile_parts = 1;
   p.tile_slots = tokens * group / 128 + n_seq + 1;
   if (p.tile) {
-    // Two workgroups on every compute unit, from the rows that there are; slots beside them stay
-    // empty.  A prompt has no more keys than tokens; a split has at least 512.  (512 tokens after
-    // 60,007, 2 heads of 128: 8 parts 312 us, 4 415, 16 327, unsplit 1,380; 256 after 8,000, 8
-    // heads: 8 parts 62, 4 73, 16 77, unsplit 197; 64 after 30,000: 32 parts 63, 16 68.
-    // Splitting only the longest tiles of a step of mixed lengths cost more in partial results,
-    // 345 us, than it evened out, 280.)
+    // Two workgroups on every compute unit, from the rows that there are; slots beside them, one a
+    // sequence and head, stay empty but count towards the 2,048 workgroups.  A prompt has no more
+    // keys than tokens; a split has at least 512.  (512 tokens after 60,007, 2 heads of 128: 8 parts
+    // 312 us, 4 415, 16 327, unsplit 1,380; 256 after 8,000, 8 heads: 8 parts 62, 4 73, 16 77,
+    // unsplit 197; 64 after 30,000: 32 parts 63, 16 68.  Splitting only the longest tiles of a step
+    // of mixed lengths cost more in partial results, 345 us, than it evened out, 280.)
     const int64_t tiles = (tokens * group + 127) / 128 * o.kv_heads;
     const int64_t slots = p.tile_slots * o.kv_heads;
     int64_t parts = 512 / tiles;
