@@ -48,9 +48,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Before the first visible key: every finite score replaces it.
 constexpr float kNoMax = -3.0e38f;
 constexpr float kLn2 = 0.69314718055994531f;
-// How far below the running maximum m is taken (log2).
+// How far below the running maximum m is taken (log2).  For bf16, whose values reach fp32's largest,
+// it lies above by what m may lag behind in the tiles: weights are 1 at most, and O overflows no
+// sooner than the formula's sum does.
 template <typename ET>
-constexpr float kBias = std::is_same<ET, _Float16>::value ? 10.0f : 0.0f;
+constexpr float kBias = std::is_same<ET, _Float16>::value ? 10.0f : -8.0f;
 // Where |t| is larger, the rounding of t itself takes up the room that is left to fp16's 2^16: there
 // m is the maximum as it is.
 constexpr float kFar = 1048576.0f;

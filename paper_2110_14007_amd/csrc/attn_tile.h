@@ -11,8 +11,8 @@
 // Bound by the matrix and vector instructions that a SIMD's two waves issue: a
 // stage is 16 MFMAs (14.3 ns each from one SIMD), 16 exponentials a lane (4.6)
 // and some 60 other vector instructions (2.1), and the clock falls to 1.75 GHz
-// under them.  One prompt of 16,001 tokens, 32 heads of 128, takes 1.91 to 2.03 ms on
-// three cards: 1,100 to 1,035 TFLOP/s of bf16, where an 8192^3 matrix product
+// under them.  One prompt of 16,001 tokens, 32 heads of 128, takes 1.87 to 2.03 ms on
+// four cards: 1,120 to 1,035 TFLOP/s of bf16, where an 8192^3 matrix product
 // reaches 1,182.  32 rows a wave
 // leave room for two workgroups a compute unit, whose waves fill each other's
 // gaps; 64 rows a wave halve the LDS reads, but need all 512 registers and were
@@ -31,8 +31,8 @@ constexpr int kKeys = 32;           // keys of a stage
 constexpr int kRing = 4;            // stages of K, and of V, in LDS
 constexpr uint32_t kNoLoad = ~0u;   // offset of a lane that loads nothing
 // Growth of the maximum (log2) that m may lag behind.  With kBias the weights stay below 2^15.5 in
-// fp16, whose numbers end at 2^16, and below 2^8 in bf16.  (512 tokens after 60,007, 2 heads of 128,
-// fp16: 287 us, without a bias 280.)
+// fp16, whose numbers end at 2^16, and at 1 at most in bf16.  (512 tokens after 60,007, 2 heads of
+// 128, fp16: 287 us, without a bias 280.)
 template <typename ET>
 constexpr float kSlack = std::is_same<ET, _Float16>::value ? 5.5f : 8.0f;
 
