@@ -597,6 +597,101 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
                           int64_t max_fresh, void* workspace, size_t ws_bytes, void* stream,
                           void* out, float* lse_out);
 
+/*
+ * Appends: a step's new keys and values into the cache with the position
+ * rotation applied on the way, and the rotated queries.  Of the first `rotary`
+ * = r elements of a head, the pairs (x_i, x_{i + r/2}), or with `interleaved`
+ * (x_2i, x_2i+1), i < r / 2, turn by the angle t = pos * rates[i]:
+ *   (x, y) -> (x cos t - y sin t, x sin t + y cos t)
+ * The angle and its cosine and sine are formed in 64 bits (the product is exact
+ * below 2^53).  Values and the elements from r on are not rotated.
+ */
+typedef struct {
+  uint32_t struct_size; /* must be sizeof(tod_append) */
+  int32_t precision;    /* of q, k, v and q_out: TOD_PREC_FP16 or TOD_PREC_BF16 */
+  int32_t heads;        /* query heads */
+  int32_t kv_heads;     /* key / value heads */
+  int32_t dim;          /* elements of a head: a multiple of 8, at most 256 */
+  int32_t rotary;       /* rotated elements of a head: even, at most dim; 0: none */
+  int32_t interleaved;  /* 1: pairs of neighbours; 0: pairs rotary / 2 apart */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+                        /* strides as in tod_attn */
+} tod_append;
+
+void tod_default_append(tod_append* append, int32_t heads, int32_t kv_heads, int32_t dim,
+                        int32_t precision);
+
+/*
+ * Append to a paged cache of 16-bit rows.
+ *   q [tokens, heads, dim], k, v [tokens, kv_heads, dim]; 16-byte aligned
+ *   pos[tokens] int32: positions, as of tod_page_map (any sign: a row of q whose
+ *                 token has no slot is rotated as every other)
+ *   rates[rotary / 2] fp32 (device): angle of a step of one position; NULL if
+ *                 rotary is 0
+ *   slot, k_pages, v_pages: as in tod_page_write
+ *   q_out [tokens, heads, dim] contiguous, sharing no memory with q, k or v
+ * Rotated elements are fp32 sums of two products, rounded once.
+ */
+tod_status tod_page_append(const tod_append* append, const void* q, const void* k, const void* v,
+                           int64_t tokens, const int32_t* pos, const float* rates,
+                           const int64_t* slot, void* k_pages, void* v_pages, int64_t n_pages,
+                           int32_t page_rows, void* stream, void* q_out);
+
+/*
+ * A paged cache of 4-bit rows: 4.25 bits an element.  A row's elements come in
+ * blocks of 32.  Element i of a row is the code in byte i / 2 of the row, its low
+ * half where i is even: codes 0 .. 7 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6, and
+ * 8 + c for the negative of c.  Byte b of a block scales them by 2^(b - 127);
+ * with 255 all of them are NaN.  An operator takes the values as numbers of its
+ * tensors' type (beyond its largest: infinite).
+ * dim is a multiple of 32; table and slots are as over 16-bit pages.
+ */
+typedef struct {
+  uint32_t struct_size; /* must be sizeof(tod_cache4) */
+  int32_t page_rows;
+  int64_t n_pages;
+  void *k_codes, *v_codes;       /* [n_pages, kv_heads, page_rows, dim / 2], 16-byte aligned */
+  uint8_t *k_scales, *v_scales;  /* [n_pages, kv_heads, page_rows, dim / 32] */
+} tod_cache4;
+
+/*
+ * Append to a 4-bit cache; arguments as in tod_page_append.  For a block whose
+ * largest magnitude is a, the scale is the smallest 2^e with a <= 7 2^e, e cut to
+ * [-23, 13] for fp16 and to [-125, 125] for bf16 (so that every value is one of
+ * the type); each element over 2^e is rounded to the nearest value, ties to
+ * the even code, beyond 6 to 6.  A block that holds an infinity or a NaN gets the byte 255
+ * and the codes 0.  Rotated keys are scaled and rounded in 64 bits, without a
+ * rounding to 16 bits before.  Of a slot that several tokens share, codes and
+ * scales may come from different ones.
+ */
+tod_status tod_page_append4(const tod_append* append, const void* q, const void* k, const void* v,
+                            int64_t tokens, const int32_t* pos, const float* rates,
+                            const int64_t* slot, const tod_cache4* cache, void* stream,
+                            void* q_out);
+
+/*
+ * Rows of a 4-bit cache as 16-bit elements: k_out, v_out [tokens, kv_heads, dim],
+ * contiguous and 16-byte aligned.  Tokens whose slot is outside the cache get zeros.
+ */
+tod_status tod_page_read4(const tod_cache4* cache, int32_t kv_heads, int32_t dim,
+                          int32_t precision, const int64_t* slot, int64_t tokens, void* stream,
+                          void* k_out, void* v_out);
+
+/*
+ * tod_attn_paged over a 4-bit cache: the same formulas, over the values that the
+ * codes stand for, and the same outputs and rules.  attn->dim is a multiple
+ * of 32; attn->precision is that of q and out.
+ * Workspace: tod_attn_paged4_workspace_size(attn, tokens, n_seq, max_fresh) bytes,
+ * 256-byte aligned (0: invalid sizes); nothing in it lasts beyond the call.
+ */
+size_t tod_attn_paged4_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_seq,
+                                      int64_t max_fresh);
+tod_status tod_attn_paged4(const tod_attn* attn, const void* q, const tod_cache4* cache,
+                           const int32_t* table, int64_t table_cols, const int32_t* row_start,
+                           const int32_t* cached, int64_t n_seq, int64_t tokens,
+                           int64_t max_fresh, void* workspace, size_t ws_bytes, void* stream,
+                           void* out, float* lse_out);
+
 /* Static string naming a status code. */
 const char* tod_status_string(tod_status status);
 

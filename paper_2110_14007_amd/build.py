@@ -12,8 +12,9 @@ LIB = os.path.join(HERE, "libtod.so")
 SOURCES = ["api.hip", "prep.hip", "select.hip", "lof.hip", "tile_f32.hip", "tile_f16.hip",
            "tile_bf16.hip", "mtile_f16.hip", "mtile_bf16.hip", "order.hip",
            "rtile_f16.hip", "rtile_bf16.hip", "nwr.hip", "score.hip", "loci.hip",
-           "pages.hip", "seq_api.hip", "attn_tile_f16.hip",
-           "attn_tile_bf16.hip", "attn_token_f16.hip", "attn_token_bf16.hip"]
+           "pages.hip", "append.hip", "seq_api.hip", "attn_tile_f16.hip",
+           "attn_tile_bf16.hip", "attn_tile4_f16.hip", "attn_tile4_bf16.hip",
+           "attn_token_f16.hip", "attn_token_bf16.hip"]
 # The fused tile kernels take maxima of MFMA accumulators (fmax, so that the
 # compiler sees the reads and inserts the wait states an MFMA result needs
 # before a VALU reads it).  Their operands are never NaN (prep rejects
@@ -24,8 +25,8 @@ NO_NAN_SOURCES = {"mtile_f16.hip", "mtile_bf16.hip", "tile_f32.hip", "tile_f16.h
                   "tile_bf16.hip",
                   # (attention: scores may be NaN.  The maximum leaves them out, exp2 and the
                   # sums carry them to the output; nothing compares them with themselves.)
-                  "attn_tile_f16.hip", "attn_tile_bf16.hip", "attn_token_f16.hip",
-                  "attn_token_bf16.hip"}
+                  "attn_tile_f16.hip", "attn_tile_bf16.hip", "attn_tile4_f16.hip",
+                  "attn_tile4_bf16.hip", "attn_token_f16.hip", "attn_token_bf16.hip"}
 # The attention kernels keep their accumulators in VGPRs (the softmax works on them between two
 # products): left to itself the compiler puts the MFMA results of a kernel that needs more than
 # 256 registers in AGPRs and copies every score and rescaled accumulator.

@@ -33,6 +33,7 @@
 
 #include "mtile.h"
 #include "seq.h"
+#include "seq4.h"
 
 namespace tod {
 namespace attn {
@@ -343,8 +344,9 @@ __device__ __forceinline__ bool met_nonfinite(const f32x16 (&o)[N], float sum) {
 // finite among the keys j0 .. j1 - 1, its output is their sum, since all weights are positive.
 // (The products do not say so: a value may have been cleared, or met a weight or a half of one that
 // was rounded to 0.)  Rows whose weights are NaN, so that `sum` is, stay NaN.  step 0: rows of the
-// output; else partial results of the rows one after the other, step elements each.
-template <typename ET, int DP, bool PAGED, typename OT, typename ST>
+// output; else partial results of the rows one after the other, step elements each.  FOUR: the
+// values are a 4-bit cache's.
+template <typename ET, int DP, bool PAGED, bool FOUR = false, typename OT, typename ST>
 __device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step, const Seq& s,
                                                   int32_t m0, int32_t j0, int32_t j1, float sum) {
   const AttnArgs& a = st.a;
@@ -375,10 +377,19 @@ __device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step,
             const uint32_t pg = div_by((uint32_t)key, a.page);
             const int32_t id = a.table[(int64_t)st.seq * a.cols + pg];
             const bool none = id < 0 || id >= a.n_pages;  // zeros
-            p += (((int64_t)id * a.kv_heads + st.head) * a.page.d +
-                  (key - (int32_t)(pg * a.page.d))) * a.dim;
-            const uint16_t* const from = (const uint16_t*)p + e;
-            u[k] = *(none ? (const uint16_t*)&kZeros : from);
+            const int64_t row = ((int64_t)id * a.kv_heads + st.head) * a.page.d +
+                                (key - (int32_t)(pg * a.page.d));
+            if constexpr (FOUR) {
+              const uint8_t* const c = (const uint8_t*)a.v + row * (a.dim / 2) + e / 2;
+              const uint8_t* const b = a.v_scales + row * (a.dim / 32) + e / 32;
+              const uint32_t code = *(none ? (const uint8_t*)&kZeros : c);
+              const uint32_t scale = *(none ? (const uint8_t*)&kZeros : b);
+              u[k] = (uint16_t)(two_values<ET, 0>(code, scale_of(scale)) >> (16 * (e & 1)));
+            } else {
+              p += row * a.dim;
+              const uint16_t* const from = (const uint16_t*)p + e;
+              u[k] = *(none ? (const uint16_t*)&kZeros : from);
+            }
           } else {
             p += (int64_t)(s.start + key) * a.v_row + (int64_t)st.head * a.v_head;
             u[k] = ((const uint16_t*)p)[e];

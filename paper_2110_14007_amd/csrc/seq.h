@@ -48,6 +48,30 @@ struct PageWriteArgs {
   int32_t kv_heads;
 };
 
+// Pages of 16-bit rows, or codes of 4-bit rows with their scales.
+struct AppendArgs {
+  const void *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
+  const int32_t* pos;
+  const float* rates;  // [rotary / 2]
+  const int64_t* slot;
+  void *q_out, *k_pages, *v_pages;
+  uint8_t *k_scales, *v_scales;
+  int64_t tokens, slots;  // slots: n_pages * page
+  FastDiv page, per_row;  // 8-element pieces of a head's row
+  int32_t heads, kv_heads, rotary, interleaved;
+};
+
+struct Read4Args {
+  const void *k_codes, *v_codes;
+  const uint8_t *k_scales, *v_scales;
+  const int64_t* slot;
+  void *k_out, *v_out;
+  int64_t tokens, slots;
+  FastDiv page, per_token, per_row;  // 8-element pieces of a token and of one head's row
+  int32_t kv_heads;
+};
+
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
@@ -73,6 +97,7 @@ struct AttnArgs {
   int32_t part_keys;    // fewest keys of a split
   float2* tile_stat;    // [tiles of all heads, parts, rows]
   float* tile_o;        // [tiles of all heads, parts, rows, padded dim]
+  const uint8_t *k_scales, *v_scales;  // of a 4-bit cache, whose codes are k and v
 };
 
 // Packed rows that the token kernel takes: a product's 32 columns.  (96 tokens over caches of 100
@@ -85,8 +110,12 @@ constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
+hipError_t launch_append(const AppendArgs& a, bool half, bool four, hipStream_t s);
+hipError_t launch_read4(const Read4Args& a, bool half, hipStream_t s);
 hipError_t launch_attn_tile_f16(const AttnArgs& a, bool paged, hipStream_t s);
 hipError_t launch_attn_tile_bf16(const AttnArgs& a, bool paged, hipStream_t s);
+hipError_t launch_attn_tile4_f16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_tile4_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_f16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_join_f16(const AttnArgs& a, hipStream_t s);

@@ -36,6 +36,13 @@ tod_status check_pages(int64_t n_pages, int32_t page_rows, int64_t kv_heads) {
   return TOD_OK;
 }
 
+tod_status check_half(int32_t precision) {
+  if (precision == TOD_PREC_FP16 || precision == TOD_PREC_BF16) return TOD_OK;
+  return precision == TOD_PREC_FP32 || precision == TOD_PREC_AUTO
+             ? unsupported("sequence operators take fp16 or bf16 tensors")
+             : invalid("unknown precision");
+}
+
 // Sizes, types and strides that all attention calls share.  rows: the row and
 // head strides that *a leaves 0 become those of a contiguous [rows, heads, dim].
 tod_status check_attn(const tod_attn* a, tod_attn* out) {
@@ -43,10 +50,8 @@ tod_status check_attn(const tod_attn* a, tod_attn* out) {
   if (a->struct_size != sizeof(tod_attn))
     return invalid("tod_attn.struct_size does not match this library");
   *out = *a;
-  if (a->precision != TOD_PREC_FP16 && a->precision != TOD_PREC_BF16)
-    return a->precision == TOD_PREC_FP32 || a->precision == TOD_PREC_AUTO
-               ? unsupported("attention takes fp16 or bf16 tensors")
-               : invalid("unknown precision");
+  const tod_status st = check_half(a->precision);
+  if (st != TOD_OK) return st;
   if (a->heads <= 0 || a->kv_heads <= 0 || a->dim <= 0)
     return invalid("heads, kv_heads and dim must be positive");
   if (a->heads % a->kv_heads)
@@ -109,8 +114,11 @@ struct Plan {
   size_t line, token_stat, token_o, tile_stat, tile_o, total;
 };
 
-// paged: the call may hold sequences of few tokens for the token kernel.
-Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fresh, bool paged) {
+enum class Form { kPrompt, kPaged, kPaged4 };  // whole prompts; pages; pages of a 4-bit cache
+
+// Over pages a call may hold sequences of few tokens for the token kernel.
+Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fresh, Form form) {
+  const bool paged = form != Form::kPrompt;
   Plan p;
   memset(&p, 0, sizeof(p));
   const int64_t group = o.heads / o.kv_heads;
@@ -122,8 +130,8 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
     at += (size_t)((bytes + 255) / 256 * 256);
     return here;
   };
-  p.tile = !paged || most > tod::kTokenMaxRows;
-  if (paged && group <= tod::kTokenMaxRows) {
+  p.tile = form != Form::kPaged || most > tod::kTokenMaxRows;
+  if (form == Form::kPaged && group <= tod::kTokenMaxRows) {
     p.skip_rows = (int32_t)(most < tod::kTokenMaxRows ? most : tod::kTokenMaxRows / group * group);
     const int64_t rows = 2 * tod::token_workers(o.dim) * p.skip_rows;
     p.line = take((n_seq + 1) * 8);
@@ -160,7 +168,7 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
   return p;
 }
 
-tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool paged, void* ws,
+tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, Form form, void* ws,
                     size_t ws_bytes, void* stream, const char* where) {
   if (!p.fits) return unsupported("too many rows for one call");
   if (!aligned(ws, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
@@ -183,13 +191,125 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, bool pag
   const bool half = o.precision == TOD_PREC_FP16;
   hipError_t e = hipSuccess;
   // The tile kernel's launch holds the token workers too.
-  if (p.tile)
+  const bool paged = form == Form::kPaged;
+  if (form == Form::kPaged4)
+    e = half ? tod::launch_attn_tile4_f16(*a, s) : tod::launch_attn_tile4_bf16(*a, s);
+  else if (p.tile)
     e = half ? tod::launch_attn_tile_f16(*a, paged, s) : tod::launch_attn_tile_bf16(*a, paged, s);
   else
     e = half ? tod::launch_attn_token_f16(*a, s) : tod::launch_attn_token_bf16(*a, s);
   if (e == hipSuccess && p.skip_rows)
     e = half ? tod::launch_attn_token_join_f16(*a, s) : tod::launch_attn_token_join_bf16(*a, s);
   return launched(e, where);
+}
+
+// What attention over pages of either kind shares: the checks and the arguments beside the pages'.
+tod_status over_pages(const tod_attn& o, const void* q, int64_t n_pages, int32_t page_rows,
+                      const int32_t* table, int64_t table_cols, const int32_t* row_start,
+                      const int32_t* cached, int64_t n_seq, int64_t tokens, int64_t max_fresh,
+                      void* workspace, void* out, float* lse_out, tod::AttnArgs* a) {
+  if (!q || !table || !row_start || !cached || !out || !workspace) return invalid("null pointer");
+  if (!o.causal) return unsupported("attention over pages is causal");
+  tod_status st = check_rows(o, tokens, n_seq);
+  if (st != TOD_OK) return st;
+  if ((st = check_pages(n_pages, page_rows, o.kv_heads)) != TOD_OK) return st;
+  if (table_cols <= 0 || max_fresh <= 0)
+    return invalid("table_cols and max_fresh must be positive");
+  if (table_cols > (kMaxCount - kBeyond - tokens) / page_rows)
+    return unsupported("positions that do not fit into 32 bits");
+  if (!aligned(q, 16) || !aligned(out, 16)) return invalid("tensors must be 16-byte aligned");
+  if (!aligned(table, 4) || !aligned(row_start, 4) || !aligned(cached, 4) || !aligned(lse_out, 4))
+    return invalid("misaligned pointer");
+  a->q = q;
+  a->row_start = row_start;
+  a->cached = cached;
+  a->table = table;
+  a->cols = table_cols;
+  a->n_pages = (int32_t)n_pages;
+  a->page = tod::fast_div((uint32_t)page_rows);
+  a->n_seq = (int32_t)n_seq;
+  a->tokens = (int32_t)tokens;
+  a->out = out;
+  a->lse = lse_out;
+  return TOD_OK;
+}
+
+tod_status check_cache4(const tod_cache4* c) {
+  if (!c) return invalid("null tod_cache4");
+  if (c->struct_size != sizeof(tod_cache4))
+    return invalid("tod_cache4.struct_size does not match this library");
+  if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return invalid("null pointer");
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16))
+    return invalid("codes must be 16-byte aligned");
+  return TOD_OK;
+}
+
+// Whether the rows of x [tokens, heads, dim], by their strides, share memory with the contiguous out.
+bool overlap(const void* x, int64_t row, int64_t head, int64_t tokens, int32_t heads, int32_t dim,
+             const void* out, int64_t out_bytes) {
+  typedef unsigned __int128 u128;  // (strides may be anything)
+  const u128 a = (uintptr_t)x, b = (uintptr_t)out;
+  const u128 n = 2 * ((u128)(tokens - 1) * (u128)row + (u128)(heads - 1) * (u128)head + (u128)dim);
+  return a < b + (u128)out_bytes && b < a + n;
+}
+
+// Checks and arguments that both appends share.
+tod_status check_append(const tod_append* o, const void* q, const void* k, const void* v,
+                        int64_t tokens, const int32_t* pos, const float* rates,
+                        const int64_t* slot, int64_t n_pages, int32_t page_rows, void* q_out,
+                        tod::AppendArgs* a) {
+  if (!o) return invalid("null tod_append");
+  if (o->struct_size != sizeof(tod_append))
+    return invalid("tod_append.struct_size does not match this library");
+  tod_status st = check_half(o->precision);
+  if (st != TOD_OK) return st;
+  if (tokens <= 0 || o->heads <= 0 || o->kv_heads <= 0 || o->dim <= 0)
+    return invalid("tokens, heads, kv_heads and dim must be positive");
+  if (o->dim % 8) return unsupported("dim must be a multiple of 8");
+  if (o->dim > 256) return unsupported("dim > 256");
+  if (o->rotary < 0 || o->rotary > o->dim || o->rotary % 2)
+    return invalid("rotary must be even and in [0, dim]");
+  if (o->interleaved != 0 && o->interleaved != 1) return invalid("interleaved must be 0 or 1");
+  if (!q || !k || !v || !pos || !slot || !q_out || (o->rotary && !rates))
+    return invalid("null pointer");
+  if ((st = check_pages(n_pages, page_rows, o->kv_heads)) != TOD_OK) return st;
+  // A token's pieces count in 32 bits; strides as 64-bit products.
+  if ((int64_t)o->heads + 2 * (int64_t)o->kv_heads > 65536 || tokens > kMaxCount)
+    return unsupported("more than 65536 heads of queries, keys and values, or 2^31 - 1 tokens");
+  memset(a, 0, sizeof(*a));
+  const int64_t given[6] = {o->q_row, o->q_head, o->k_row, o->k_head, o->v_row, o->v_head};
+  int64_t* const to[6] = {&a->q_row, &a->q_head, &a->k_row, &a->k_head, &a->v_row, &a->v_head};
+  for (int i = 0; i < 6; ++i) {
+    if (given[i] < 0) return invalid("strides must not be negative");
+    if (given[i] % 8) return unsupported("strides must be multiples of 8 elements");
+    *to[i] = given[i] ? given[i]
+                      : i % 2 ? o->dim : (int64_t)o->dim * (i == 0 ? o->heads : o->kv_heads);
+  }
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16))
+    return invalid("tensors must be 16-byte aligned");
+  if (!aligned(pos, 4) || !aligned(rates, 4) || !aligned(slot, 8))
+    return invalid("misaligned pointer");
+  const int64_t out_bytes = 2 * tokens * o->heads * o->dim;
+  if (overlap(q, a->q_row, a->q_head, tokens, o->heads, o->dim, q_out, out_bytes) ||
+      overlap(k, a->k_row, a->k_head, tokens, o->kv_heads, o->dim, q_out, out_bytes) ||
+      overlap(v, a->v_row, a->v_head, tokens, o->kv_heads, o->dim, q_out, out_bytes))
+    return invalid("q_out shares memory with an input");
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->pos = pos;
+  a->rates = rates;
+  a->slot = slot;
+  a->q_out = q_out;
+  a->tokens = tokens;
+  a->slots = n_pages * page_rows;
+  a->page = tod::fast_div((uint32_t)page_rows);
+  a->per_row = tod::fast_div((uint32_t)(o->dim / 8));
+  a->heads = o->heads;
+  a->kv_heads = o->kv_heads;
+  a->rotary = o->rotary;
+  a->interleaved = o->interleaved;
+  return TOD_OK;
 }
 
 }  // namespace
@@ -288,8 +408,8 @@ size_t tod_attn_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_s
   tod_attn o;
   if (check_attn(attn, &o) != TOD_OK || check_rows(o, tokens, n_seq) != TOD_OK || max_fresh <= 0)
     return 0;
-  const Plan paged = make_plan(o, tokens, n_seq, max_fresh, true);
-  const Plan prompt = make_plan(o, tokens, n_seq, max_fresh, false);
+  const Plan paged = make_plan(o, tokens, n_seq, max_fresh, Form::kPaged);
+  const Plan prompt = make_plan(o, tokens, n_seq, max_fresh, Form::kPrompt);
   const size_t a = paged.fits ? paged.total : 0, b = prompt.fits ? prompt.total : 0;
   return a > b ? a : b;
 }
@@ -317,8 +437,8 @@ tod_status tod_attn_prompt(const tod_attn* attn, const void* q, const void* k, c
   a.tokens = (int32_t)tokens;
   a.out = out;
   a.lse = lse_out;
-  return run_attn(o, &a, make_plan(o, tokens, n_seq, tokens, false), false, workspace, ws_bytes,
-                  stream, "tod_attn_prompt");
+  return run_attn(o, &a, make_plan(o, tokens, n_seq, tokens, Form::kPrompt), Form::kPrompt,
+                  workspace, ws_bytes, stream, "tod_attn_prompt");
 }
 
 tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pages,
@@ -331,36 +451,139 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
   tod_attn o;
   tod_status st = check_attn(attn, &o);
   if (st != TOD_OK) return st;
-  if (!q || !k_pages || !v_pages || !table || !row_start || !cached || !out || !workspace)
-    return invalid("null pointer");
-  if (!o.causal) return unsupported("attention over pages is causal");
-  if ((st = check_rows(o, tokens, n_seq)) != TOD_OK) return st;
-  if ((st = check_pages(n_pages, page_rows, o.kv_heads)) != TOD_OK) return st;
-  if (table_cols <= 0 || max_fresh <= 0)
-    return invalid("table_cols and max_fresh must be positive");
-  if (table_cols > (kMaxCount - kBeyond - tokens) / page_rows)
-    return unsupported("positions that do not fit into 32 bits");
-  if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+  if (!k_pages || !v_pages) return invalid("null pointer");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
     return invalid("tensors must be 16-byte aligned");
-  if (!aligned(table, 4) || !aligned(row_start, 4) || !aligned(cached, 4) || !aligned(lse_out, 4))
-    return invalid("misaligned pointer");
   tod::AttnArgs a;
   fill(o, &a);
-  a.q = q;
   a.k = k_pages;
   a.v = v_pages;
-  a.row_start = row_start;
-  a.cached = cached;
-  a.table = table;
-  a.cols = table_cols;
-  a.n_pages = (int32_t)n_pages;
-  a.page = tod::fast_div((uint32_t)page_rows);
-  a.n_seq = (int32_t)n_seq;
-  a.tokens = (int32_t)tokens;
-  a.out = out;
-  a.lse = lse_out;
-  return run_attn(o, &a, make_plan(o, tokens, n_seq, max_fresh, true), true, workspace, ws_bytes,
-                  stream, "tod_attn_paged");
+  st = over_pages(o, q, n_pages, page_rows, table, table_cols, row_start, cached, n_seq, tokens,
+                  max_fresh, workspace, out, lse_out, &a);
+  if (st != TOD_OK) return st;
+  return run_attn(o, &a, make_plan(o, tokens, n_seq, max_fresh, Form::kPaged), Form::kPaged,
+                  workspace, ws_bytes, stream, "tod_attn_paged");
+}
+
+void tod_default_append(tod_append* a, int32_t heads, int32_t kv_heads, int32_t dim,
+                        int32_t precision) {
+  if (!a) return;
+  memset(a, 0, sizeof(*a));
+  a->struct_size = sizeof(*a);
+  a->precision = precision;
+  a->heads = heads;
+  a->kv_heads = kv_heads;
+  a->dim = dim;
+  a->rotary = dim;
+}
+
+tod_status tod_page_append(const tod_append* append, const void* q, const void* k, const void* v,
+                           int64_t tokens, const int32_t* pos, const float* rates,
+                           const int64_t* slot, void* k_pages, void* v_pages, int64_t n_pages,
+                           int32_t page_rows, void* stream, void* q_out) {
+  set_error(TOD_OK, "");
+  tod::AppendArgs a;
+  const tod_status st = check_append(append, q, k, v, tokens, pos, rates, slot, n_pages, page_rows,
+                                     q_out, &a);
+  if (st != TOD_OK) return st;
+  if (!k_pages || !v_pages) return invalid("null pointer");
+  if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
+    return invalid("tensors must be 16-byte aligned");
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  return launched(tod::launch_append(a, append->precision == TOD_PREC_FP16, false,
+                                     (hipStream_t)stream), "tod_page_append");
+}
+
+tod_status tod_page_append4(const tod_append* append, const void* q, const void* k, const void* v,
+                            int64_t tokens, const int32_t* pos, const float* rates,
+                            const int64_t* slot, const tod_cache4* cache, void* stream,
+                            void* q_out) {
+  set_error(TOD_OK, "");
+  tod_status st = check_cache4(cache);
+  if (st != TOD_OK) return st;
+  tod::AppendArgs a;
+  st = check_append(append, q, k, v, tokens, pos, rates, slot, cache->n_pages, cache->page_rows,
+                    q_out, &a);
+  if (st != TOD_OK) return st;
+  if (append->dim % 32) return unsupported("dim must be a multiple of 32");
+  a.k_pages = cache->k_codes;
+  a.v_pages = cache->v_codes;
+  a.k_scales = cache->k_scales;
+  a.v_scales = cache->v_scales;
+  return launched(tod::launch_append(a, append->precision == TOD_PREC_FP16, true,
+                                     (hipStream_t)stream), "tod_page_append4");
+}
+
+tod_status tod_page_read4(const tod_cache4* cache, int32_t kv_heads, int32_t dim,
+                          int32_t precision, const int64_t* slot, int64_t tokens, void* stream,
+                          void* k_out, void* v_out) {
+  set_error(TOD_OK, "");
+  tod_status st = check_cache4(cache);
+  if (st != TOD_OK) return st;
+  if (!slot || !k_out || !v_out) return invalid("null pointer");
+  if (tokens <= 0 || kv_heads <= 0 || dim <= 0)
+    return invalid("tokens, kv_heads and dim must be positive");
+  if ((st = check_half(precision)) != TOD_OK) return st;
+  if (dim % 32) return unsupported("dim must be a multiple of 32");
+  if (dim > 256) return unsupported("dim > 256");
+  if ((st = check_pages(cache->n_pages, cache->page_rows, kv_heads)) != TOD_OK) return st;
+  const int64_t per_token = (int64_t)(dim / 8) * kv_heads;
+  if (per_token > kMaxCount || tokens > (kMaxCount - 256) / per_token)
+    return unsupported("more than 2^31 - 1 pieces of 16 bytes in one call");
+  if (!aligned(k_out, 16) || !aligned(v_out, 16))
+    return invalid("tensors must be 16-byte aligned");
+  if (!aligned(slot, 8)) return invalid("misaligned pointer");
+  tod::Read4Args a;
+  a.k_codes = cache->k_codes;
+  a.v_codes = cache->v_codes;
+  a.k_scales = cache->k_scales;
+  a.v_scales = cache->v_scales;
+  a.slot = slot;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.tokens = tokens;
+  a.slots = cache->n_pages * cache->page_rows;
+  a.page = tod::fast_div((uint32_t)cache->page_rows);
+  a.per_token = tod::fast_div((uint32_t)per_token);
+  a.per_row = tod::fast_div((uint32_t)(dim / 8));
+  a.kv_heads = kv_heads;
+  return launched(tod::launch_read4(a, precision == TOD_PREC_FP16, (hipStream_t)stream),
+                  "tod_page_read4");
+}
+
+size_t tod_attn_paged4_workspace_size(const tod_attn* attn, int64_t tokens, int64_t n_seq,
+                                      int64_t max_fresh) {
+  tod_attn o;
+  if (check_attn(attn, &o) != TOD_OK || check_rows(o, tokens, n_seq) != TOD_OK || max_fresh <= 0 ||
+      o.dim % 32)
+    return 0;
+  const Plan p = make_plan(o, tokens, n_seq, max_fresh, Form::kPaged4);
+  return p.fits ? p.total : 0;
+}
+
+tod_status tod_attn_paged4(const tod_attn* attn, const void* q, const tod_cache4* cache,
+                           const int32_t* table, int64_t table_cols, const int32_t* row_start,
+                           const int32_t* cached, int64_t n_seq, int64_t tokens,
+                           int64_t max_fresh, void* workspace, size_t ws_bytes, void* stream,
+                           void* out, float* lse_out) {
+  set_error(TOD_OK, "");
+  tod_attn o;
+  tod_status st = check_attn(attn, &o);
+  if (st != TOD_OK) return st;
+  if (o.dim % 32) return unsupported("dim must be a multiple of 32");
+  if ((st = check_cache4(cache)) != TOD_OK) return st;
+  tod::AttnArgs a;
+  fill(o, &a);
+  a.k = cache->k_codes;
+  a.v = cache->v_codes;
+  a.k_scales = cache->k_scales;
+  a.v_scales = cache->v_scales;
+  st = over_pages(o, q, cache->n_pages, cache->page_rows, table, table_cols, row_start, cached,
+                  n_seq, tokens, max_fresh, workspace, out, lse_out, &a);
+  if (st != TOD_OK) return st;
+  return run_attn(o, &a, make_plan(o, tokens, n_seq, max_fresh, Form::kPaged4), Form::kPaged4,
+                  workspace, ws_bytes, stream, "tod_attn_paged4");
 }
 
 }  // extern "C"

@@ -35,7 +35,10 @@ SYMBOLS = ("tod_default_options", "tod_workspace_size", "tod_knn", "tod_knn_noal
            "tod_nwr", "tod_loci_workspace_size", "tod_loci",
            "tod_plan", "tod_plan_workspace", "tod_page_map", "tod_page_write",
            "tod_default_attn", "tod_attn_workspace_size", "tod_attn_prompt", "tod_attn_paged",
-           "tod_status_string", "tod_last_error")
+           "tod_default_append", "tod_page_append", "tod_status_string", "tod_last_error")
+# Those of a 4-bit cache.
+SYMBOLS4 = ("tod_page_append4", "tod_page_read4", "tod_attn_paged4_workspace_size",
+            "tod_attn_paged4")
 
 
 class tod_options(ctypes.Structure):
@@ -105,6 +108,36 @@ class tod_attn(ctypes.Structure):
         ("k_head", ctypes.c_int64),
         ("v_row", ctypes.c_int64),
         ("v_head", ctypes.c_int64),
+    ]
+
+
+class tod_append(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("precision", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("rotary", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("q_row", ctypes.c_int64),
+        ("q_head", ctypes.c_int64),
+        ("k_row", ctypes.c_int64),
+        ("k_head", ctypes.c_int64),
+        ("v_row", ctypes.c_int64),
+        ("v_head", ctypes.c_int64),
+    ]
+
+
+class tod_cache4(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("page_rows", ctypes.c_int32),
+        ("n_pages", ctypes.c_int64),
+        ("k_codes", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
     ]
 
 
@@ -178,6 +211,20 @@ def _load():
     lib.tod_attn_paged.argtypes = [at_p, vp, vp, vp, i64, i32, vp, i64, vp, vp, i64, i64, i64, vp,
                                    sz, vp, vp, vp]
     lib.tod_attn_paged.restype = ctypes.c_int
+    ap_p, c4_p = ctypes.POINTER(tod_append), ctypes.POINTER(tod_cache4)
+    lib.tod_default_append.argtypes = [ap_p, i32, i32, i32, i32]
+    lib.tod_default_append.restype = None
+    lib.tod_page_append.argtypes = [ap_p, vp, vp, vp, i64, vp, vp, vp, vp, vp, i64, i32, vp, vp]
+    lib.tod_page_append.restype = ctypes.c_int
+    lib.tod_page_append4.argtypes = [ap_p, vp, vp, vp, i64, vp, vp, vp, c4_p, vp, vp]
+    lib.tod_page_append4.restype = ctypes.c_int
+    lib.tod_page_read4.argtypes = [c4_p, i32, i32, i32, vp, i64, vp, vp, vp]
+    lib.tod_page_read4.restype = ctypes.c_int
+    lib.tod_attn_paged4_workspace_size.argtypes = [at_p, i64, i64, i64]
+    lib.tod_attn_paged4_workspace_size.restype = sz
+    lib.tod_attn_paged4.argtypes = [at_p, vp, c4_p, vp, i64, vp, vp, i64, i64, i64, vp, sz, vp, vp,
+                                    vp]
+    lib.tod_attn_paged4.restype = ctypes.c_int
     lib.tod_status_string.argtypes = [ctypes.c_int]
     lib.tod_status_string.restype = ctypes.c_char_p
     lib.tod_last_error.argtypes = []
@@ -980,6 +1027,198 @@ def tod_attn_paged(q, k_pages, v_pages, table, row_start, cached, max_fresh=None
            page_rows, table.data_ptr(), cols, row_start.data_ptr(), cached.data_ptr(), n, tokens,
            fresh, buf.data_ptr(), buf.numel(), _STREAM, out.data_ptr(),
            lse.data_ptr() if return_lse else None)
+    return (out, lse) if return_lse else out
+
+
+class Cache4:
+    """A paged key / value cache of 4-bit rows, from its tensors (contiguous, uint8):
+
+    k_codes, v_codes [n_pages, kv_heads, page_rows, dim / 2]: two codes a byte, the even element's
+    in the low half; k_scales, v_scales [n_pages, kv_heads, page_rows, dim / 32]: the scale of a
+    block of 32 elements, 2^(byte - 127).  Cache4.zeros makes them.  dim is a multiple of 32.
+    """
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        self._index = _index_of(k_codes, "k_codes")
+        u8 = (_seq().u8,)
+        for x, name in ((k_codes, "k_codes"), (k_scales, "k_scales"), (v_codes, "v_codes"),
+                        (v_scales, "v_scales")):
+            _want(x, name, u8, 4, self._index)
+        n, heads, rows, half = k_codes.shape
+        if half % 16:
+            raise ValueError("dim must be a multiple of 32")
+        if v_codes.shape != k_codes.shape or k_scales.shape != (n, heads, rows, half // 16) \
+                or v_scales.shape != k_scales.shape:
+            raise ValueError("codes must be [pages, heads, rows, dim / 2] and scales "
+                             "[pages, heads, rows, dim / 32], the same for keys and values")
+        self._tensors = (k_codes, k_scales, v_codes, v_scales)
+        self.n_pages, self.kv_heads, self.page_rows, self.dim = n, heads, rows, 2 * half
+
+    @classmethod
+    def zeros(cls, n_pages: int, kv_heads: int, page_rows: int, dim: int, device="cuda:0"):
+        torch = _torch()
+        if dim % 32:
+            raise ValueError("dim must be a multiple of 32")
+        return cls(*(torch.zeros((n_pages, kv_heads, page_rows, dim // per), dtype=torch.uint8,
+                                 device=device) for per in (2, 32, 2, 32)))
+
+    k_codes = property(lambda self: self._tensors[0])
+    k_scales = property(lambda self: self._tensors[1])
+    v_codes = property(lambda self: self._tensors[2])
+    v_scales = property(lambda self: self._tensors[3])
+
+    def _arg(self, index):
+        if self._index != index:
+            raise ValueError("the cache must be on the other tensors' device")
+        kc, ks, vc, vs = self._tensors
+        return tod_cache4(_CACHE4_SIZE, self.page_rows, self.n_pages, kc.data_ptr(), vc.data_ptr(),
+                          ks.data_ptr(), vs.data_ptr())
+
+
+_CACHE4_SIZE = ctypes.sizeof(tod_cache4)
+_APPEND_SIZE = ctypes.sizeof(tod_append)
+
+
+def _append(q, k, v, pos, slot, rates, kv_heads, dim, interleaved, stream, out):
+    """Checks that both appends share -> (device index, q_out, tod_append)."""
+    dev = _index_of(q, "q")
+    env = _seq()
+    _want(q, "q", env.half, 3, dev, False)
+    _want(k, "k", (q.dtype,), 3, dev, False)
+    _want(v, "v", (q.dtype,), 3, dev, False)
+    _want(pos, "pos", env.i32, 1, dev)
+    _want(slot, "slot", env.i64, 1, dev)
+    _want(rates, "rates", env.f32, 1, dev)
+    tokens, heads, _ = q.shape
+    if q.shape[2] != dim or k.shape != (tokens, kv_heads, dim) or v.shape != k.shape:
+        raise ValueError("q must be [tokens, heads, %d] and k and v [tokens, %d, %d] as the cache is"
+                         % (dim, kv_heads, dim))
+    if pos.shape[0] != tokens or slot.shape[0] != tokens:
+        raise ValueError("pos and slot must have one entry per token")
+    rotary = 2 * rates.shape[0]
+    if rotary > dim:
+        raise ValueError("rates must have at most dim / 2 entries")
+    (qr, qh), (kr, kh), (vr, vh) = _strides(q, "q"), _strides(k, "k"), _strides(v, "v")
+    out, _ = _attn_outputs(q, out, False, stream)
+    return dev, out, tod_append(_APPEND_SIZE, PREC_FP16 if q.dtype == env.fp16 else PREC_BF16,
+                                heads, kv_heads, dim, rotary, 1 if interleaved else 0, qr, qh, kr,
+                                kh, vr, vh)
+
+
+def tod_page_append(q, k, v, pos, slot, rates, k_pages, v_pages, interleaved: bool = False,
+                    stream=None, out=None):
+    """Rotate q and k by position, and write k and v into their slots of 16-bit pages.
+
+    q [tokens, heads, dim], k, v [tokens, kv_heads, dim] (fp16 or bf16, strides as of
+    tod_attn_prompt); pos int32 and slot int64 [tokens], as of tod_page_map; rates fp32 [r / 2]:
+    the angle of a step of one position, for the pairs (i, i + r / 2) of a head's first r elements,
+    or (2 i, 2 i + 1) with interleaved; k_pages, v_pages as in tod_page_write, written in place.
+    -> the rotated q [tokens, heads, dim]
+    """
+    _, kv_heads, page_rows, dim = _pages(k_pages, v_pages, _seq().half, _index_of(q, "q"))
+    dev, out, a = _append(q, k, v, pos, slot, rates, kv_heads, dim, interleaved, stream, out)
+    if k_pages.dtype != q.dtype:
+        raise TypeError("k_pages must have q's dtype")
+    tokens = q.shape[0]
+    if tokens == 0:
+        return out
+    _queue("tod_page_append", _lib.tod_page_append, dev, stream,
+           (q, k, v, pos, slot, rates, k_pages, v_pages, out),
+           ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens, pos.data_ptr(),
+           rates.data_ptr(), slot.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+           k_pages.shape[0], page_rows, _STREAM, out.data_ptr())
+    return out
+
+
+def tod_page_append4(q, k, v, pos, slot, rates, cache, interleaved: bool = False, stream=None,
+                     out=None):
+    """Rotate q and k by position, and write k and v into their slots of a 4-bit cache (Cache4).
+
+    Arguments as in tod_page_append.  A block of 32 elements with the largest magnitude a gets the
+    smallest scale 2^e with a <= 7 2^e, and its elements the nearest of the codes' values.
+    -> the rotated q [tokens, heads, dim]
+    """
+    dev, out, a = _append(q, k, v, pos, slot, rates, cache.kv_heads, cache.dim, interleaved, stream,
+                          out)
+    c = cache._arg(dev)
+    tokens = q.shape[0]
+    if tokens == 0:
+        return out
+    _queue("tod_page_append4", _lib.tod_page_append4, dev, stream,
+           (q, k, v, pos, slot, rates, out) + cache._tensors,
+           ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(), tokens, pos.data_ptr(),
+           rates.data_ptr(), slot.data_ptr(), ctypes.byref(c), _STREAM, out.data_ptr())
+    return out
+
+
+def tod_page_read4(cache, slot, dtype, stream=None):
+    """Rows of a 4-bit cache at the slots (int64 [tokens], negative: zeros), as fp16 or bf16.
+
+    -> k, v [tokens, kv_heads, dim]
+    """
+    dev = _index_of(slot, "slot")
+    env = _seq()
+    _want(slot, "slot", env.i64, 1, dev)
+    if dtype not in env.half:
+        raise TypeError("dtype must be %s" % " or ".join(str(d) for d in env.half))
+    c = cache._arg(dev)
+    tokens = slot.shape[0]
+    out = _new(slot, (2, tokens, cache.kv_heads, cache.dim), dtype, stream)
+    k, v = out[0], out[1]
+    if tokens == 0:
+        return k, v
+    _queue("tod_page_read4", _lib.tod_page_read4, dev, stream, (slot, out) + cache._tensors,
+           ctypes.byref(c), cache.kv_heads, cache.dim,
+           PREC_FP16 if dtype == env.fp16 else PREC_BF16, slot.data_ptr(), tokens, _STREAM,
+           k.data_ptr(), v.data_ptr())
+    return k, v
+
+
+@functools.lru_cache(maxsize=1024)
+def _attn4_room(heads, kv_heads, dim, tokens, n_seq, max_fresh):
+    a = tod_attn()
+    _lib.tod_default_attn(ctypes.byref(a), heads, kv_heads, dim, PREC_FP16)
+    return int(_lib.tod_attn_paged4_workspace_size(ctypes.byref(a), tokens, n_seq, max_fresh))
+
+
+def tod_attn_paged4_workspace_size(heads: int, kv_heads: int, dim: int, tokens: int, n_seq: int,
+                                   max_fresh=None) -> int:
+    """Workspace bytes of tod_attn_paged4 (0: sizes that it refuses)."""
+    return _attn4_room(int(heads), int(kv_heads), int(dim), int(tokens), int(n_seq),
+                       int(tokens if max_fresh is None else max_fresh))
+
+
+def tod_attn_paged4(q, cache, table, row_start, cached, max_fresh=None, scale=None, workspace=None,
+                    stream=None, out=None, return_lse: bool = False):
+    """Attention of every sequence's new tokens over its pages of a 4-bit cache (Cache4).
+
+    Arguments and results as in tod_attn_paged, over the values that the cache's codes stand for.
+    """
+    dev = _index_of(q, "q")
+    env = _seq()
+    _want(q, "q", env.half, 3, dev, False)
+    _want(table, "table", env.i32, 2, dev)
+    _want(row_start, "row_start", env.i32, 1, dev)
+    _want(cached, "cached", env.i32, 1, dev)
+    tokens, heads, dim = q.shape
+    n, cols = table.shape
+    kv_heads = cache.kv_heads
+    if dim != cache.dim:
+        raise ValueError("q and the cache must have the same dim")
+    if cached.shape[0] != n or row_start.shape[0] != n + 1:
+        raise ValueError("table, row_start and cached must describe the same sequences")
+    c = cache._arg(dev)
+    a = _attn(q, kv_heads, True, scale)
+    out, lse = _attn_outputs(q, out, return_lse, stream)
+    if tokens == 0:
+        return (out, lse) if return_lse else out
+    fresh = tokens if max_fresh is None else int(max_fresh)
+    buf = _attn_ws(workspace, _attn4_room(heads, kv_heads, dim, tokens, n, fresh), q, stream)
+    _queue("tod_attn_paged4", _lib.tod_attn_paged4, dev, stream,
+           (q, table, row_start, cached, out, lse, buf) + cache._tensors,
+           ctypes.byref(a), q.data_ptr(), ctypes.byref(c), table.data_ptr(), cols,
+           row_start.data_ptr(), cached.data_ptr(), n, tokens, fresh, buf.data_ptr(), buf.numel(),
+           _STREAM, out.data_ptr(), lse.data_ptr() if return_lse else None)
     return (out, lse) if return_lse else out
 
 
