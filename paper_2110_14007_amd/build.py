@@ -14,7 +14,8 @@ SOURCES = ["api.hip", "prep.hip", "select.hip", "lof.hip", "tile_f32.hip", "tile
            "rtile_f16.hip", "rtile_bf16.hip", "nwr.hip", "score.hip", "loci.hip",
            "pages.hip", "append.hip", "seq_api.hip", "attn_tile_f16.hip",
            "attn_tile_bf16.hip", "attn_tile4_f16.hip", "attn_tile4_bf16.hip",
-           "attn_token_f16.hip", "attn_token_bf16.hip"]
+           "attn_token_f16.hip", "attn_token_bf16.hip", "attn_token4_f16.hip",
+           "attn_token4_bf16.hip"]
 # The fused tile kernels take maxima of MFMA accumulators (fmax, so that the
 # compiler sees the reads and inserts the wait states an MFMA result needs
 # before a VALU reads it).  Their operands are never NaN (prep rejects

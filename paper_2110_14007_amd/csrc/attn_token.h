@@ -39,13 +39,15 @@ constexpr int token_loads() { return 2 * kTokenKeys * DP * 2 / 1024; }
 template <int DP>
 constexpr int token_lds() { return token_ring<DP>() * 2 * kTokenKeys * DP * 2; }
 
-// Stages of a sequence that is the token kernel's, else 0.
+// Stages of KEYS keys of a sequence that is the token kernel's, else 0.
+template <int KEYS>
 __device__ __forceinline__ int32_t token_stages(const AttnArgs& a, const Seq& q) {
   if (q.n <= 0 || (int64_t)q.n * a.group.d > a.skip_rows) return 0;
-  return (q.keys + kTokenKeys - 1) / kTokenKeys;
+  return (q.keys + KEYS - 1) / KEYS;
 }
+template <int KEYS>
 __device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
-  return s < a.n_seq ? token_stages(a, seq_of<true>(a, s)) : 0;
+  return s < a.n_seq ? token_stages<KEYS>(a, seq_of<true>(a, s)) : 0;
 }
 
 // Of `all` stages worker w of `grid` (a power of two) has those from share(w) on; where there are
@@ -84,48 +86,52 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// A worker: a wave, with the LDS of its ring.
-template <typename ET, int DP>
-__device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t worker,
-                                           uint16_t* const lds) {
-  constexpr uint32_t grid = (uint32_t)token_workers(DP);
-  using V8 = typename Frag<ET>::V;
-  using St = Stager<ET, DP, true>;
-  constexpr int kStage = kTokenKeys * DP;  // elements of a K or V stage
-  constexpr int kRing = token_ring<DP>(), kLoads = token_loads<DP>(), DB = DP / 32;
-  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+// A worker's share of the line of stages, and where in it the share begins.
+struct Share {
+  int64_t at, end;  // its stages
+  int32_t s;        // the sequence that holds stage `at`
+  int64_t off;      // of `at` in the sequence's stages of all heads
+  int32_t seg;      // sequences that a lane summed; of one, what it is:
+  Seq own;
+};
 
+template <int KEYS>
+__device__ __forceinline__ Share deal(const AttnArgs& a, const uint32_t worker,
+                                      const uint32_t grid) {
+  Share w;
   // The line of stages: lane l sums the sequences of its own segment (of one, where there are no
   // more than lanes: then it holds what that sequence is).
-  const int32_t seg = (a.n_seq + 63) / 64, s0 = lane * seg;
-  const Seq own = s0 < a.n_seq ? seq_of<true>(a, s0) : Seq{0, 0, 0, 0};
-  int64_t mine = token_stages(a, own);
-  for (int32_t i = 1; i < seg; ++i) mine += token_stages(a, s0 + i);
+  const int lane = threadIdx.x & 63;
+  const int32_t seg = w.seg = (a.n_seq + 63) / 64, s0 = lane * seg;
+  w.own = s0 < a.n_seq ? seq_of<true>(a, s0) : Seq{0, 0, 0, 0};
+  int64_t mine = token_stages<KEYS>(a, w.own);
+  for (int32_t i = 1; i < seg; ++i) mine += token_stages<KEYS>(a, s0 + i);
   const int64_t incl = lane_prefix(mine);
   const int64_t all = __shfl(incl, 63, 64) * a.kv_heads;
   if (worker == 0) {  // for the join
     int64_t before = incl - mine;
     for (int32_t i = 0; i < seg && s0 + i < a.n_seq; ++i) {
       a.token_line[s0 + i] = before;
-      before += i == 0 ? token_stages(a, own) : token_stages(a, s0 + i);
+      before += i == 0 ? token_stages<KEYS>(a, w.own) : token_stages<KEYS>(a, s0 + i);
     }
     if (lane == 63) a.token_line[a.n_seq] = incl;
   }
   // This worker's share of it.
-  int64_t at = share(worker, all, grid), end = share(worker + 1, all, grid);
-  if (end > all) at = end = all;
+  w.at = share(worker, all, grid);
+  w.end = share(worker + 1, all, grid);
+  if (w.end > all) w.at = w.end = all;
 
   // The sequence that holds stage `at`: its segment, then 64 sequences a step.
-  int32_t s = 0;
-  int64_t off = 0;  // of `at` in the sequence's stages of all heads
-  if (at < end) {
-    const int64_t target = quotient(at, a.kv_heads);
+  w.s = 0;
+  w.off = 0;
+  if (w.at < w.end) {
+    const int64_t target = quotient(w.at, a.kv_heads);
     const int L = __popcll(__ballot(incl - mine <= target)) - 1;
     int64_t before = __shfl(incl - mine, L, 64);
     int32_t first = L * seg;
-    s = first;
+    int32_t s = first;
     while (seg > 1) {
-      const int32_t c = first + lane < (L + 1) * seg ? token_stages(a, first + lane) : 0;
+      const int32_t c = first + lane < (L + 1) * seg ? token_stages<KEYS>(a, first + lane) : 0;
       const int64_t in = lane_prefix(c);
       const int64_t sum = __shfl(in, 63, 64);
       if (target < before + sum) {
@@ -137,19 +143,54 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
       before += sum;
       first += 64;
     }
-    s = __builtin_amdgcn_readfirstlane(s);
-    off = at - before * a.kv_heads;
+    w.s = __builtin_amdgcn_readfirstlane(s);
+    w.off = w.at - before * a.kv_heads;
   }
+  return w;
+}
+
+// The sequence of number s: from the lane that summed it, or from memory.
+__device__ __forceinline__ Seq dealt(const AttnArgs& a, const Share& w, int32_t s) {
+  if (w.seg == 1)
+    return {__builtin_amdgcn_readlane(w.own.start, s), __builtin_amdgcn_readlane(w.own.n, s),
+            __builtin_amdgcn_readlane(w.own.keys, s), __builtin_amdgcn_readlane(w.own.shift, s)};
+  return seq_of<true>(a, s);
+}
+
+// Rows past the last sequence, where no tile kernel takes them.
+__device__ __forceinline__ void clear_tail(const AttnArgs& a, const uint32_t worker,
+                                           const uint32_t grid) {
+  if (!a.token_tail) return;
+  const int lane = threadIdx.x & 63;
+  const int32_t words = a.heads * a.dim / 8;
+  for (int32_t t = start_of(a, a.n_seq) + (int32_t)worker; t < a.tokens; t += (int32_t)grid) {
+    for (int32_t i = lane; i < words; i += 64)
+      ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
+    if (a.lse)
+      for (int32_t i = lane; i < a.heads; i += 64) a.lse[(int64_t)t * a.heads + i] = -INFINITY;
+  }
+}
+
+// A worker: a wave, with the LDS of its ring.
+template <typename ET, int DP>
+__device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t worker,
+                                           uint16_t* const lds) {
+  constexpr uint32_t grid = (uint32_t)token_workers(DP);
+  using V8 = typename Frag<ET>::V;
+  using St = Stager<ET, DP, true>;
+  constexpr int kStage = kTokenKeys * DP;  // elements of a K or V stage
+  constexpr int kRing = token_ring<DP>(), kLoads = token_loads<DP>(), DB = DP / 32;
+  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+
+  const Share mine = deal<kTokenKeys>(a, worker, grid);
+  int64_t at = mine.at, off = mine.off;
+  const int64_t end = mine.end;
+  int32_t s = mine.s;
 
   const uint32_t base = mt::lds_off(lds);
   for (bool opening = true; at < end; opening = false) {
-    Seq sq;
-    if (seg == 1)
-      sq = {__builtin_amdgcn_readlane(own.start, s), __builtin_amdgcn_readlane(own.n, s),
-            __builtin_amdgcn_readlane(own.keys, s), __builtin_amdgcn_readlane(own.shift, s)};
-    else
-      sq = seq_of<true>(a, s);
-    const int32_t stages = token_stages(a, sq);
+    const Seq sq = dealt(a, mine, s);
+    const int32_t stages = token_stages<kTokenKeys>(a, sq);
     if (stages == 0) {  // another kernel's, or idle
       ++s;
       off = 0;
@@ -287,17 +328,7 @@ __device__ __forceinline__ void token_work(const AttnArgs& a, const uint32_t wor
     }
   }
 
-  // Rows past the last sequence, where no tile kernel takes them.
-  if (a.token_tail) {
-    const int32_t words = a.heads * a.dim / 8;
-    for (int32_t t = start_of(a, a.n_seq) + (int32_t)worker; t < a.tokens;
-         t += (int32_t)grid) {
-      for (int32_t i = lane; i < words; i += 64)
-        ((uint4*)a.out)[(int64_t)t * words + i] = uint4{0, 0, 0, 0};
-      if (a.lse)
-        for (int32_t i = lane; i < a.heads; i += 64) a.lse[(int64_t)t * a.heads + i] = -INFINITY;
-    }
-  }
+  clear_tail(a, worker, grid);
 }
 
 template <typename ET, int DP>
@@ -310,9 +341,8 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
 // takes one of its packed rows, and each wave an equal part of the row's pieces.  Otherwise it
 // takes all of the pair's rows, a wave a row at a time.
 constexpr int kJoinWaves = 8;
-template <typename ET, int DP, bool ALL>
+template <typename ET, int DP, bool ALL, uint32_t grid>
 __global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a) {
-  constexpr uint32_t grid = (uint32_t)token_workers(DP);
   const uint32_t row = ALL ? blockIdx.x % (uint32_t)a.skip_rows : 0;
   const uint32_t pair = ALL ? blockIdx.x / (uint32_t)a.skip_rows : blockIdx.x;
   const uint32_t s = div_by(pair, a.heads_div), head = pair - s * a.heads_div.d;
@@ -368,18 +398,18 @@ hipError_t launch_token(const AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename ET, int DP>
+template <typename ET, int DP, uint32_t grid>
 hipError_t launch_token_join(const AttnArgs& a, hipStream_t s) {
   // A pair has some workers / pairs pieces; from 16 on a workgroup a row joins them sooner (2
   // sequences of 20,000 to 32,000 tokens, 2 heads: the whole call 24 us, with a wave a row 50), and
   // below that a wave a row (16 of 3,000 to 9,000, 8 heads: 75.6 us, with a workgroup a row 77.4).
   const int64_t pairs = (int64_t)a.n_seq * a.kv_heads;
   const unsigned rows = (unsigned)a.skip_rows;
-  if (16 * pairs <= token_workers(DP))
-    hipLaunchKernelGGL((token_join_kernel<ET, DP, true>), dim3((unsigned)pairs * rows),
+  if (16 * pairs <= (int64_t)grid)
+    hipLaunchKernelGGL((token_join_kernel<ET, DP, true, grid>), dim3((unsigned)pairs * rows),
                        dim3(64 * kJoinWaves), 0, s, a);
   else
-    hipLaunchKernelGGL((token_join_kernel<ET, DP, false>), dim3((unsigned)pairs),
+    hipLaunchKernelGGL((token_join_kernel<ET, DP, false, grid>), dim3((unsigned)pairs),
                        dim3(64 * (rows < kJoinWaves ? rows : kJoinWaves)), 0, s, a);
   return hipGetLastError();
 }

@@ -1,0 +1,389 @@
+// Attention of few new tokens a sequence over a 4-bit cache: bound by the bytes
+// of codes and scales, each read once.
+//
+// The line of stages and its workers are those of attn_token.h, with stages of
+// 64 keys (32 for more than 128 elements) and two waves on every SIMD.  A quarter
+// of the bytes of 16-bit rows leaves a wave a quarter of the time for a key,
+// so that its arithmetic is laid out for few instructions:
+//
+// * v_mfma_f32_16x16x32: 16 keys by 16 packed rows, half the columns of the
+//   larger product, which few rows leave empty anyway.  In both operands lane l
+//   holds row l % 16 and eight elements of the contraction, in any order that is the
+//   same on both sides; of the result it holds column l % 16, rows
+//   4 (l / 16) + r.
+// * Keys go from memory to registers: lane l loads 16 bytes of key l % 16, the
+//   block l / 16 of its row, which is one scale and the operand of four products
+//   after 16 conversions.  (A row of 64 elements: eight bytes, half a block.)
+//   The stage after is in flight meanwhile.
+// * Values are loaded the same way, converted with their block's scale, written to
+//   the wave's own LDS as 32 rows of 16-bit elements and read by the transposing
+//   read as the second product's operand.
+// * The scores of two blocks of keys are its other operand right from the
+//   accumulators: lane l holds keys 4 (l / 16) + r of each, and the values are read
+//   in that order.
+//
+// Softmax, halves of the weights and values that are not finite: as in attn.h and
+// attn_token.h.
+#pragma once
+
+#include "attn_token.h"
+
+namespace tod {
+namespace attn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename ET>
+__device__ __forceinline__ f32x4 mfma16(typename Frag<ET>::V a, typename Frag<ET>::V b, f32x4 c) {
+  if constexpr (std::is_same<ET, _Float16>::value)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <typename F>
+__device__ __forceinline__ float over_quarters(float v, F&& f) {
+  const uint32_t u = __float_as_uint(v);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t w = __float_as_uint(f(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const auto q = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// Growth of the maximum (log2) that m may lag behind.  With kBias the weights stay below 2^15.5 in
+// fp16, whose numbers end at 2^16, and at 1 at most in bf16.
+template <typename ET>
+constexpr float kSlack4 = std::is_same<ET, _Float16>::value ? 5.5f : 8.0f;
+
+template <int DP>
+constexpr int token4_tiles() { return DP == 256 ? 2 : 4; }  // blocks of 16 keys of a stage
+template <int DP>
+constexpr int token4_keys() { return 16 * token4_tiles<DP>(); }
+
+// Stage of 32 rows of values: piece c of row r at c ^ swizzle.  A wave writes 16 rows at one piece and
+// reads, with each 16 lanes, two pieces of four rows.
+template <int DP>
+__device__ __forceinline__ int swizzle4(int row) {
+  if constexpr (DP == 64)
+    return (row >> 1 & 3) << 1 | (row >> 3 & 1);
+  else
+    return (row & 3) << 1 | (row >> 2 & 1) | (row & 8);
+}
+
+// A lane's codes of a stage's keys or values.  Words: of a row; scales: one for four words.
+template <int DP>
+struct Lane4 {
+  static constexpr int kWords = DP / 32, kScales = DP == 256 ? 2 : 1, kTiles = token4_tiles<DP>();
+  uint32_t w[kTiles][kWords];
+  uint32_t scale[kTiles][kScales];
+};
+
+// First element of word i of lane group g's codes of a row.
+template <int DP>
+__device__ __forceinline__ int element4(int i, int g) {
+  if constexpr (DP == 64)
+    return 16 * g + 8 * i;
+  else
+    return 32 * (g + 4 * (i / 4)) + 8 * (i % 4);
+}
+
+// A worker: a wave, with LDS for 32 rows of values.  NB: blocks of 16 packed rows that it keeps.
+template <typename ET, int DP, int NB>
+__device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t worker,
+                                            uint16_t* const lds) {
+  constexpr uint32_t grid = (uint32_t)token4_workers(DP);
+  constexpr int KT = token4_tiles<DP>(), KEYS = token4_keys<DP>(), C = DP / 32, DB = DP / 16;
+  using V8 = typename Frag<ET>::V;
+  using L4 = Lane4<DP>;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+
+  const Share mine = deal<KEYS>(a, worker, grid);
+  int64_t at = mine.at, off = mine.off;
+  const int64_t end = mine.end;
+  int32_t s = mine.s;
+
+  for (bool opening = true; at < end; opening = false) {
+    const Seq sq = dealt(a, mine, s);
+    const int32_t stages = token_stages<KEYS>(a, sq);
+    if (stages == 0) {  // another kernel's, or idle
+      ++s;
+      off = 0;
+      continue;
+    }
+    const uint32_t head = (uint32_t)quotient(off, stages);
+    const int32_t jb = (int32_t)(off - (int64_t)head * stages);
+    const int32_t je = (int32_t)min((int64_t)stages, jb + (end - at));
+
+    const int32_t rows = sq.n * (int32_t)a.group.d;
+    int32_t tok[NB], qh[NB], limit[NB];
+    V8 q[NB][C];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int32_t m = min(16 * b + n, rows - 1);
+      tok[b] = (int32_t)div_by((uint32_t)m, a.group);
+      qh[b] = (int32_t)head * (int32_t)a.group.d + m - tok[b] * (int32_t)a.group.d;
+      limit[b] = min(sq.shift + tok[b], sq.keys - 1);
+      const ET* const p =
+          (const ET*)a.q + (int64_t)(sq.start + tok[b]) * a.q_row + (int64_t)qh[b] * a.q_head;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int e = element4<DP>(c, g);
+        u32x4 w = *(const u32x4*)(p + (e < a.dim ? e : 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = e < a.dim ? w[i] : 0u;
+        q[b][c] = __builtin_bit_cast(V8, w);
+      }
+    }
+    const int32_t wlo = __builtin_amdgcn_readfirstlane(limit[0]);
+
+    Stager<ET, DP, true> st(a, head);
+    st.seq = s;
+    st.start = sq.start;
+    st.seen = sq.keys;
+    auto load = [&](int32_t j, L4& k, L4& v) __attribute__((always_inline)) {
+      const uint32_t pl = st.place(j * KEYS, KEYS);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        const uint32_t row = (uint32_t)__shfl((int)pl, 16 * t + n, 64);
+#pragma unroll
+        for (int i = 0; i < L4::kScales; ++i) {
+          constexpr int kBytes = DP == 64 ? 8 : 16;
+          typedef uint32_t words __attribute__((ext_vector_type(kBytes / 4)));
+          const int e = element4<DP>(4 * i, g);
+          const bool ok = row != ~0u && e < a.dim;
+          const int64_t to = (int64_t)row * (a.dim / 2) + e / 2;
+          const int64_t sc = (int64_t)row * (a.dim / 32) + e / 32;
+          const uint8_t* const zeros = (const uint8_t*)&kZeros;
+          const words kw =
+              __builtin_nontemporal_load((const words*)(ok ? (const uint8_t*)a.k + to : zeros));
+          const words vw =
+              __builtin_nontemporal_load((const words*)(ok ? (const uint8_t*)a.v + to : zeros));
+#pragma unroll
+          for (int x = 0; x < kBytes / 4; ++x) {
+            k.w[t][4 * i + x] = kw[x];
+            v.w[t][4 * i + x] = vw[x];
+          }
+          k.scale[t][i] = *(ok ? a.k_scales + sc : zeros);
+          v.scale[t][i] = *(ok ? a.v_scales + sc : zeros);
+        }
+      }
+    };
+
+    f32x4 o[DB][NB];
+    float mref[NB], limit_raw[NB];  // a score above limit_raw makes mref follow
+    Sum acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d][b] = f32x4{0, 0, 0, 0};
+      mref[b] = kNoMax;
+      limit_raw[b] = -INFINITY;
+    }
+    bool cleared = false;  // values that are not finite were taken for 0
+
+    auto turn = [&](int32_t j, const L4& k, const L4& v) __attribute__((always_inline)) {
+      const int32_t j0 = j * KEYS;
+      f32x4 x[KT][NB];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) x[t][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const V8 f = __builtin_bit_cast(
+              V8, eight_values<ET>(k.w[t][c], scale_of(k.scale[t][DP == 64 ? 0 : c / 4])));
+#pragma unroll
+          for (int b = 0; b < NB; ++b) x[t][b] = mfma16<ET>(f, q[b][c], x[t][b]);
+        }
+      }
+      const bool edge = j0 + KEYS - 1 > wlo;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (edge) {
+          const int32_t left = limit[b] - j0 - 4 * g;
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (16 * t + r > left) x[t][b][r] = -INFINITY;
+        }
+        float top = x[0][b][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, x[t][b][r]);
+        if (__ballot(top > limit_raw[b])) {
+          // m follows the maximum only when that has grown by more than kSlack4.
+          constexpr float kRoom = kSlack4<ET> + kBias<ET>;
+          const float raw = over_quarters(top, [](float p, float r) { return fmaxf(p, r); });
+          const float t2 = raw * a.scale;
+          const bool far = fabsf(fmaxf(t2, mref[b])) > kFar;  // m follows every growth
+          const float next =
+              t2 > mref[b] + (far ? 0.0f : kRoom) ? t2 - (far ? 0.0f : kBias<ET>) : mref[b];
+          const float f = __builtin_amdgcn_exp2f(mref[b] - next);
+          mref[b] = next;
+          limit_raw[b] = far ? fmaxf(raw, limit_raw[b]) : (next + kRoom) * a.unscale;
+          acc[b].scale(f);
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[d][b][r] *= f;
+        }
+        float part = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            x[t][b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][b][r], a.scale, -mref[b]));
+            part += x[t][b][r];
+          }
+        acc[b].add(part);
+      }
+#pragma unroll
+      for (int u = 0; u < KT / 2; ++u) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int row = 16 * t + n;
+#pragma unroll
+          for (int i = 0; i < L4::kWords; ++i)
+            *(u32x4*)(lds + row * DP + 8 * ((element4<DP>(i, g) / 8) ^ swizzle4<DP>(row))) =
+                eight_values<ET>(v.w[2 * u + t][i],
+                                 scale_of(v.scale[2 * u + t][DP == 64 ? 0 : i / 4]));
+        }
+        // (One wave's LDS accesses are done in order.)
+        asm volatile("" ::: "memory");
+        // A value that is not finite must not meet the zero weight of a row that does not see it.
+        if (edge && rows > (int32_t)a.group.d && holds_nonfinite<ET, DP>(lds)) {
+          clear_nonfinite<ET, DP>(lds, 0, 64);
+          cleared = true;
+        }
+        V8 hi[NB], lo[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          typedef ET e8 __attribute__((ext_vector_type(8)));
+          e8 h, l;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p = x[2 * u + e / 4][b][e % 4];
+            h[e] = (ET)p;
+            l[e] = (ET)(p - (float)h[e]);
+          }
+          hi[b] = __builtin_bit_cast(V8, h);
+          lo[b] = __builtin_bit_cast(V8, l);
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int row = 4 * g + n / 4;
+          const int piece = 2 * d + ((n & 3) >> 1), within = 4 * (n & 1);
+          typedef __attribute__((address_space(3))) s16x4* lds4;
+          const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds4)(lds + row * DP + 8 * (piece ^ swizzle4<DP>(row)) + within));
+          const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds4)(lds + (row + 16) * DP + 8 * (piece ^ swizzle4<DP>(row + 16)) + within));
+          const V8 f = __builtin_bit_cast(
+              V8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            o[d][b] = mfma16<ET>(f, hi[b], o[d][b]);
+            o[d][b] = mfma16<ET>(f, lo[b], o[d][b]);
+          }
+        }
+        asm volatile("" ::: "memory");
+      }
+    };
+
+    // The loads of the stage after are in flight while one is worked on.
+    L4 k0, v0, k1, v1;
+    load(jb, k0, v0);
+    for (int32_t j = jb; j < je; j += 2) {
+      if (j + 1 < je) load(j + 1, k1, v1);
+      __builtin_amdgcn_sched_barrier(0);
+      turn(j, k0, v0);
+      if (j + 1 >= je) break;
+      if (j + 2 < je) load(j + 2, k0, v0);
+      __builtin_amdgcn_sched_barrier(0);
+      turn(j + 1, k1, v1);
+    }
+
+    float sum[NB];
+    bool restore = cleared;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      sum[b] = over_quarters(acc[b].v, [](float p, float r) { return p + r; });
+      float all = 0.0f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) all += fabsf(o[d][b][r]);
+      restore |= __ballot(!finite(all) && finite(sum[b])) != 0;
+    }
+    const float own_sum = NB == 2 && (lane & 16) ? sum[NB - 1] : sum[0];  // of row lane % 32
+
+    const bool whole = jb == 0 && je == stages;
+    // At most two of a worker's pieces are not whole: its first and its last.
+    const int64_t row0 = (2 * (int64_t)worker + !opening) * a.skip_rows;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int32_t m = 16 * b + n;
+      if (m >= rows) continue;
+      const int64_t orow = (int64_t)(sq.start + tok[b]) * a.heads + qh[b];
+      if (whole) {
+        if (a.lse && g == 0) a.lse[orow] = log_sum(mref[b], sum[b]);
+        const float f = inverse(sum[b]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int e = 16 * d + 4 * g;
+          if (e >= a.dim) break;
+          uint2 w;
+          w.x = pack2<ET>(o[d][b][0] * f, o[d][b][1] * f);
+          w.y = pack2<ET>(o[d][b][2] * f, o[d][b][3] * f);
+          *(uint2*)((ET*)a.out + orow * a.dim + e) = w;
+        }
+      } else {
+        if (g == 0) a.token_stat[row0 + m] = {mref[b], sum[b]};
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          *(f32x4*)(a.token_o + (row0 + m) * DP + 16 * d + 4 * g) = o[d][b];
+      }
+    }
+    if (restore) {
+      if (whole)
+        restore_nonfinite<ET, DP, true, true>(st, (ET*)a.out, 0, sq, 0, 0, sq.keys, own_sum);
+      else
+        restore_nonfinite<ET, DP, true, true>(st, a.token_o + row0 * DP, DP, sq, 0, jb * KEYS,
+                                              je * KEYS, own_sum);
+    }
+    at += je - jb;
+    off += je - jb;
+    if (off == (int64_t)stages * a.kv_heads) {
+      ++s;
+      off = 0;
+    }
+  }
+  clear_tail(a, worker, grid);
+}
+
+template <typename ET, int DP, int NB>
+__global__ void __launch_bounds__(64, DP == 256 || NB == 2 ? 1 : 2) token4_kernel(AttnArgs a) {
+  __shared__ __align__(16) uint16_t lds[32 * DP];
+  token4_work<ET, DP, NB>(a, blockIdx.x, lds);
+}
+
+template <typename ET, int DP>
+hipError_t launch_token4(const AttnArgs& a, hipStream_t s) {
+  const auto kern = a.skip_rows <= 16 ? token4_kernel<ET, DP, 1> : token4_kernel<ET, DP, 2>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)token4_workers(DP)), dim3(64), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_token_join<ET, DP, (uint32_t)token4_workers(DP)>(a, s);
+}
+
+template <typename ET>
+hipError_t launch_token4(const AttnArgs& a, hipStream_t s) {
+  if (a.dim <= 64) return launch_token4<ET, 64>(a, s);
+  if (a.dim <= 128) return launch_token4<ET, 128>(a, s);
+  return launch_token4<ET, 256>(a, s);
+}
+
+}  // namespace attn
+}  // namespace tod

@@ -108,6 +108,9 @@ constexpr int kTokenMaxRows = 32;
 // TB/s with four a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
 constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
+// Over a 4-bit cache: two waves on each of 1,024 SIMDs, one for more than 128 elements.
+constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 1024 : 2048; }
+
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
 hipError_t launch_append(const AppendArgs& a, bool half, bool four, hipStream_t s);
@@ -116,6 +119,8 @@ hipError_t launch_attn_tile_f16(const AttnArgs& a, bool paged, hipStream_t s);
 hipError_t launch_attn_tile_bf16(const AttnArgs& a, bool paged, hipStream_t s);
 hipError_t launch_attn_tile4_f16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_tile4_bf16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_token4_f16(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_token4_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_f16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_bf16(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_token_join_f16(const AttnArgs& a, hipStream_t s);

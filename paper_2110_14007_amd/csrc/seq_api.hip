@@ -130,10 +130,14 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
     at += (size_t)((bytes + 255) / 256 * 256);
     return here;
   };
-  p.tile = form != Form::kPaged || most > tod::kTokenMaxRows;
-  if (form == Form::kPaged && group <= tod::kTokenMaxRows) {
-    p.skip_rows = (int32_t)(most < tod::kTokenMaxRows ? most : tod::kTokenMaxRows / group * group);
-    const int64_t rows = 2 * tod::token_workers(o.dim) * p.skip_rows;
+  p.tile = !paged || most > tod::kTokenMaxRows;
+  if (paged && group <= tod::kTokenMaxRows) {
+    // Beside tiles the workers over a 4-bit cache keep one block of 16 rows where a token fits in.
+    const bool four = form == Form::kPaged4;
+    const int64_t limit = four && p.tile && group <= 16 ? 16 : tod::kTokenMaxRows;
+    p.skip_rows = (int32_t)(most < limit ? most : limit / group * group);
+    const int64_t rows =
+        2 * (four ? tod::token4_workers(o.dim) : tod::token_workers(o.dim)) * p.skip_rows;
     p.line = take((n_seq + 1) * 8);
     p.token_stat = take(rows * 8);
     p.token_o = take(rows * dp * 4);
@@ -190,11 +194,16 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, Form for
   const hipStream_t s = (hipStream_t)stream;
   const bool half = o.precision == TOD_PREC_FP16;
   hipError_t e = hipSuccess;
-  // The tile kernel's launch holds the token workers too.
   const bool paged = form == Form::kPaged;
-  if (form == Form::kPaged4)
-    e = half ? tod::launch_attn_tile4_f16(*a, s) : tod::launch_attn_tile4_bf16(*a, s);
-  else if (p.tile)
+  if (form == Form::kPaged4) {
+    if (p.tile)
+      e = half ? tod::launch_attn_tile4_f16(*a, s) : tod::launch_attn_tile4_bf16(*a, s);
+    if (e == hipSuccess && p.skip_rows)
+      e = half ? tod::launch_attn_token4_f16(*a, s) : tod::launch_attn_token4_bf16(*a, s);
+    return launched(e, where);
+  }
+  // The tile kernel's launch holds the token workers too.
+  if (p.tile)
     e = half ? tod::launch_attn_tile_f16(*a, paged, s) : tod::launch_attn_tile_bf16(*a, paged, s);
   else
     e = half ? tod::launch_attn_token_f16(*a, s) : tod::launch_attn_token_bf16(*a, s);
