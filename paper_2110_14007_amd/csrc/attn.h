@@ -101,6 +101,18 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int32_t s) {
 // 16 zero bytes: what a lane stages for a key, or a piece of one, that does not exist.
 static __device__ const uint4 kZeros = {0, 0, 0, 0};
 
+// A load that is known to be from global memory.  Of a pointer that may be one of two the compiler
+// knows no address space, and a flat load would be waited for by every wait for an LDS access.
+template <typename T>
+__device__ __forceinline__ T load_global(const void* p) {
+  return *(const __attribute__((address_space(1))) T*)(uintptr_t)p;
+}
+// The same of data that no other wave reads.
+template <typename T>
+__device__ __forceinline__ T load_once(const void* p) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) T*)(uintptr_t)p);
+}
+
 template <typename ET>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
   typedef ET e2 __attribute__((ext_vector_type(2)));

@@ -122,12 +122,9 @@ __device__ __forceinline__ AttnArgs own_args() {
 // A wave's share of a 4-bit stage of keys or values, on its way from memory to LDS: eight rows of
 // eight lanes, DP / 8 elements a lane, all of one block.
 template <int DP>
-struct __attribute__((aligned(DP / 16))) CodeWords {
-  uint32_t w[DP / 64];
-};
-template <int DP>
 struct Codes {
-  CodeWords<DP> words;
+  typedef uint32_t W __attribute__((ext_vector_type(DP / 64)));
+  W words;
   uint32_t scale;
 };
 
@@ -267,8 +264,8 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     const uint8_t* const c = (const uint8_t*)(isk ? a.k : a.v) + (int64_t)row * (dim / 2) + e4 / 2;
     const uint8_t* const b = (isk ? a.k_scales : a.v_scales) + (int64_t)row * (dim / 32) + e4 / 32;
     Codes<DP>& to = isk ? kcodes : vcodes;
-    to.words = *(const CodeWords<DP>*)(ok ? c : (const uint8_t*)&kZeros);
-    to.scale = *(ok ? b : (const uint8_t*)&kZeros);
+    to.words = load_global<typename Codes<DP>::W>(ok ? c : (const uint8_t*)&kZeros);
+    to.scale = load_global<uint8_t>(ok ? b : (const uint8_t*)&kZeros);
   };
   auto put = [&](auto ISK, int32_t i, int ring) __attribute__((always_inline)) {
     constexpr bool isk = decltype(ISK)::value;
@@ -279,7 +276,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     const float scale = scale_of(from.scale);
 #pragma unroll
     for (int x = 0; x < DP / 64; ++x)
-      *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>(from.words.w[x], scale);
+      *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>((uint32_t)from.words[x], scale);
   };
 
   f32x16 o[DB];

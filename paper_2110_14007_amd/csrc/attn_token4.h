@@ -155,17 +155,15 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
           const int64_t to = (int64_t)row * (a.dim / 2) + e / 2;
           const int64_t sc = (int64_t)row * (a.dim / 32) + e / 32;
           const uint8_t* const zeros = (const uint8_t*)&kZeros;
-          const words kw =
-              __builtin_nontemporal_load((const words*)(ok ? (const uint8_t*)a.k + to : zeros));
-          const words vw =
-              __builtin_nontemporal_load((const words*)(ok ? (const uint8_t*)a.v + to : zeros));
+          const words kw = load_once<words>(ok ? (const uint8_t*)a.k + to : zeros);
+          const words vw = load_once<words>(ok ? (const uint8_t*)a.v + to : zeros);
 #pragma unroll
           for (int x = 0; x < kBytes / 4; ++x) {
             k.w[t][4 * i + x] = kw[x];
             v.w[t][4 * i + x] = vw[x];
           }
-          k.scale[t][i] = *(ok ? a.k_scales + sc : zeros);
-          v.scale[t][i] = *(ok ? a.v_scales + sc : zeros);
+          k.scale[t][i] = load_global<uint8_t>(ok ? a.k_scales + sc : zeros);
+          v.scale[t][i] = load_global<uint8_t>(ok ? a.v_scales + sc : zeros);
         }
       }
     };
