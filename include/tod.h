@@ -650,8 +650,9 @@ typedef struct {
   uint32_t struct_size; /* must be sizeof(tod_cache4) */
   int32_t page_rows;
   int64_t n_pages;
-  void *k_codes, *v_codes;       /* [n_pages, kv_heads, page_rows, dim / 2], 16-byte aligned */
+  void *k_codes, *v_codes;       /* [n_pages, kv_heads, page_rows, dim / 2] */
   uint8_t *k_scales, *v_scales;  /* [n_pages, kv_heads, page_rows, dim / 32] */
+                                 /* all four 16-byte aligned */
 } tod_cache4;
 
 /*

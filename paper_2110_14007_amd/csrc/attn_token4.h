@@ -41,6 +41,9 @@ __device__ __forceinline__ f32x4 mfma16(typename Frag<ET>::V a, typename Frag<ET
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// A value that all lanes hold, as a scalar.
+__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 template <typename F>
 __device__ __forceinline__ float over_quarters(float v, F&& f) {
@@ -55,6 +58,22 @@ __device__ __forceinline__ float over_quarters(float v, F&& f) {
 // fp16, whose numbers end at 2^16, and at 1 at most in bf16.
 template <typename ET>
 constexpr float kSlack4 = std::is_same<ET, _Float16>::value ? 5.5f : 8.0f;
+
+// The elements of a packed pair in 32 bits.
+template <typename ET>
+__device__ __forceinline__ float low_half(uint32_t w) {
+  if constexpr (std::is_same<ET, _Float16>::value)
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)w);
+  else
+    return __uint_as_float(w << 16);
+}
+template <typename ET>
+__device__ __forceinline__ float high_half(uint32_t w) {
+  if constexpr (std::is_same<ET, _Float16>::value)
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16));
+  else
+    return __uint_as_float(w & 0xffff0000u);
+}
 
 template <int DP>
 constexpr int token4_tiles() { return DP == 256 ? 2 : 4; }  // blocks of 16 keys of a stage
@@ -71,7 +90,8 @@ __device__ __forceinline__ int swizzle4(int row) {
     return (row & 3) << 1 | (row >> 2 & 1) | (row & 8);
 }
 
-// A lane's codes of a stage's keys or values.  Words: of a row; scales: one for four words.
+// A lane's codes of a stage's keys or values: words of a row of each block of keys, and a scale for
+// four of them.
 template <int DP>
 struct Lane4 {
   static constexpr int kWords = DP / 32, kScales = DP == 256 ? 2 : 1, kTiles = token4_tiles<DP>();
@@ -89,7 +109,8 @@ __device__ __forceinline__ int element4(int i, int g) {
 }
 
 // A worker: a wave, with LDS for 32 rows of values.  NB: blocks of 16 packed rows that it keeps.
-template <typename ET, int DP, int NB>
+// EVEN: pages hold whole blocks of 16 keys, so that the wave finds a block by one address.
+template <typename ET, int DP, int NB, bool EVEN>
 __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t worker,
                                             uint16_t* const lds) {
   constexpr uint32_t grid = (uint32_t)token4_workers(DP);
@@ -104,16 +125,17 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
   int32_t s = mine.s;
 
   for (bool opening = true; at < end; opening = false) {
-    const Seq sq = dealt(a, mine, s);
+    Seq sq = dealt(a, mine, s);
+    sq = {uniform(sq.start), uniform(sq.n), uniform(sq.keys), uniform(sq.shift)};
     const int32_t stages = token_stages<KEYS>(a, sq);
     if (stages == 0) {  // another kernel's, or idle
       ++s;
       off = 0;
       continue;
     }
-    const uint32_t head = (uint32_t)quotient(off, stages);
-    const int32_t jb = (int32_t)(off - (int64_t)head * stages);
-    const int32_t je = (int32_t)min((int64_t)stages, jb + (end - at));
+    const uint32_t head = (uint32_t)uniform((int32_t)quotient(off, stages));
+    const int32_t jb = uniform((int32_t)(off - (int64_t)head * stages));
+    const int32_t je = uniform((int32_t)min((int64_t)stages, jb + (end - at)));
 
     const int32_t rows = sq.n * (int32_t)a.group.d;
     int32_t tok[NB], qh[NB], limit[NB];
@@ -135,37 +157,72 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
         q[b][c] = __builtin_bit_cast(V8, w);
       }
     }
-    const int32_t wlo = __builtin_amdgcn_readfirstlane(limit[0]);
+    const int32_t wlo = uniform(limit[0]);
 
     Stager<ET, DP, true> st(a, head);
     st.seq = s;
     st.start = sq.start;
     st.seen = sq.keys;
-    auto load = [&](int32_t j, L4& k, L4& v) __attribute__((always_inline)) {
-      const uint32_t pl = st.place(j * KEYS, KEYS);
+    // Rows of the cache of a stage's keys: of each block's first key (EVEN), or of key `lane`.  gone:
+    // blocks without a page.
+    uint32_t block[KT], each = 0, gone = 0;
+    auto find = [&](int32_t j) __attribute__((always_inline)) {
+      if constexpr (EVEN) {
+        gone = 0;
 #pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        const uint32_t row = (uint32_t)__shfl((int)pl, 16 * t + n, 64);
-#pragma unroll
-        for (int i = 0; i < L4::kScales; ++i) {
-          constexpr int kBytes = DP == 64 ? 8 : 16;
-          typedef uint32_t words __attribute__((ext_vector_type(kBytes / 4)));
-          const int e = element4<DP>(4 * i, g);
-          const bool ok = row != ~0u && e < a.dim;
-          const int64_t to = (int64_t)row * (a.dim / 2) + e / 2;
-          const int64_t sc = (int64_t)row * (a.dim / 32) + e / 32;
-          const uint8_t* const zeros = (const uint8_t*)&kZeros;
-          const words kw = load_once<words>(ok ? (const uint8_t*)a.k + to : zeros);
-          const words vw = load_once<words>(ok ? (const uint8_t*)a.v + to : zeros);
-#pragma unroll
-          for (int x = 0; x < kBytes / 4; ++x) {
-            k.w[t][4 * i + x] = kw[x];
-            v.w[t][4 * i + x] = vw[x];
-          }
-          k.scale[t][i] = load_global<uint8_t>(ok ? a.k_scales + sc : zeros);
-          v.scale[t][i] = load_global<uint8_t>(ok ? a.v_scales + sc : zeros);
+        for (int t = 0; t < KT; ++t) {
+          const uint32_t row = (uint32_t)uniform((int32_t)st.row_of(j * KEYS + 16 * t));
+          gone |= row == ~0u ? 1u << t : 0u;
+          block[t] = row == ~0u ? 0u : row;
         }
+      } else {
+        each = st.place(j * KEYS, KEYS);
       }
+    };
+    // Loads of block t.  There is no branch around them: they are waited for by their number.  What is
+    // loaded for a block without a page (the cache's first rows) is cleared in its turn.
+    const uint32_t row_bytes = (uint32_t)a.dim / 2, row_scales = (uint32_t)a.dim / 32;
+    auto load = [&](const void* codes, const uint8_t* scales, L4& to, int t)
+        __attribute__((always_inline)) {
+      constexpr int kBytes = DP == 64 ? 8 : 16;
+      typedef uint32_t words __attribute__((ext_vector_type(kBytes / 4)));
+      const uint32_t row = EVEN ? 0u : (uint32_t)__shfl((int)each, 16 * t + n, 64);
+#pragma unroll
+      for (int i = 0; i < L4::kScales; ++i) {
+        const int e = element4<DP>(4 * i, g);
+        const uint8_t *c, *b;
+        if constexpr (EVEN) {
+          const uint32_t in = e < a.dim ? (uint32_t)e : 0u;
+          c = (const uint8_t*)codes + (uint64_t)block[t] * row_bytes + (n * row_bytes + in / 2);
+          b = scales + (uint64_t)block[t] * row_scales + ((n * row_scales + in / 32) & ~3u);
+        } else {
+          const bool ok = row != ~0u && e < a.dim;
+          const uint8_t* const zeros = (const uint8_t*)&kZeros;
+          c = ok ? (const uint8_t*)codes + (uint64_t)row * row_bytes + (uint32_t)e / 2 : zeros;
+          b = ok ? scales + (uint64_t)row * row_scales + (uint32_t)e / 32 : zeros;
+        }
+        const words w = load_once<words>(c);
+#pragma unroll
+        for (int x = 0; x < kBytes / 4; ++x) to.w[t][4 * i + x] = w[x];
+        to.scale[t][i] = EVEN ? load_global<uint32_t>(b) : load_global<uint8_t>(b);
+      }
+    };
+    // The scales of a block's 16 rows come as whole words: a byte loaded for the next turn would be
+    // extended, and so waited for, at the end of this one.
+    auto scale_in = [&](const L4& x, int t, int i) __attribute__((always_inline)) {
+      const int e = element4<DP>(4 * i, g);
+      const uint32_t in = e < a.dim ? (uint32_t)e : 0u;
+      return scale_of(EVEN ? x.scale[t][i] >> (8 * ((n * row_scales + in / 32) & 3)) & 0xff
+                           : x.scale[t][i]);
+    };
+    // Clears what is no code: of a key that is out, or of a lane past a row's last element.
+    auto clear = [&](L4& x, int t, bool out) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < L4::kWords; ++i)
+        x.w[t][i] = out || element4<DP>(i, g) >= a.dim ? 0u : x.w[t][i];
+#pragma unroll
+      for (int i = 0; i < L4::kScales; ++i)
+        x.scale[t][i] = out || element4<DP>(4 * i, g) >= a.dim ? 0u : x.scale[t][i];
     };
 
     f32x4 o[DB][NB];
@@ -180,20 +237,39 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
     }
     bool cleared = false;  // values that are not finite were taken for 0
 
-    auto turn = [&](int32_t j, const L4& k, const L4& v) __attribute__((always_inline)) {
+    L4 k, v;
+    auto turn = [&](int32_t j, auto MORE) __attribute__((always_inline)) {
+      constexpr bool more = decltype(MORE)::value;  // a stage follows: its loads are issued
       const int32_t j0 = j * KEYS;
+      const uint32_t none = gone;  // of this stage
       f32x4 x[KT][NB];
+      const bool narrow = a.dim < DP;  // some lanes have no element
+      if (none || narrow) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) clear(k, t, none >> t & 1);
+      }
+      float scale[KT][L4::kScales];
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) x[t][b] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < L4::kScales; ++i) scale[t][i] = scale_in(k, t, i);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const V8 f = __builtin_bit_cast(
-              V8, eight_values<ET>(k.w[t][c], scale_of(k.scale[t][DP == 64 ? 0 : c / 4])));
+        for (int b = 0; b < NB; ++b) x[t][b] = f32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          const V8 f = __builtin_bit_cast(V8, eight_values<ET>(k.w[t][c], scale[t][c / 4]));
 #pragma unroll
           for (int b = 0; b < NB; ++b) x[t][b] = mfma16<ET>(f, q[b][c], x[t][b]);
         }
+      if constexpr (more) {
+        find(j + 1);
+        __builtin_amdgcn_sched_barrier(0);  // into the registers that the conversions left
+#pragma unroll
+        for (int t = 0; t < KT; ++t) load(a.k, a.k_scales, k, t);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const bool edge = j0 + KEYS - 1 > wlo;
 #pragma unroll
@@ -238,71 +314,92 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
           }
         acc[b].add(part);
       }
+      if (edge || none || narrow) {
+        // No value that does not exist may meet a weight, not even one of 0.
+#pragma unroll
+        for (int t = 0; t < KT; ++t) clear(v, t, (none >> t & 1) || j0 + 16 * t + n >= sq.keys);
+      }
 #pragma unroll
       for (int u = 0; u < KT / 2; ++u) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int row = 16 * t + n;
+          float scale[L4::kScales];
+#pragma unroll
+          for (int i = 0; i < L4::kScales; ++i) scale[i] = scale_in(v, 2 * u + t, i);
 #pragma unroll
           for (int i = 0; i < L4::kWords; ++i)
             *(u32x4*)(lds + row * DP + 8 * ((element4<DP>(i, g) / 8) ^ swizzle4<DP>(row))) =
-                eight_values<ET>(v.w[2 * u + t][i],
-                                 scale_of(v.scale[2 * u + t][DP == 64 ? 0 : i / 4]));
+                eight_values<ET>(v.w[2 * u + t][i], scale[i / 4]);
+        }
+        if constexpr (more) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) load(a.v, a.v_scales, v, 2 * u + t);
+          __builtin_amdgcn_sched_barrier(0);
         }
         // (One wave's LDS accesses are done in order.)
         asm volatile("" ::: "memory");
         // A value that is not finite must not meet the zero weight of a row that does not see it.
-        if (edge && rows > (int32_t)a.group.d && holds_nonfinite<ET, DP>(lds)) {
-          clear_nonfinite<ET, DP>(lds, 0, 64);
-          cleared = true;
-        }
-        V8 hi[NB], lo[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          typedef ET e8 __attribute__((ext_vector_type(8)));
-          e8 h, l;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float p = x[2 * u + e / 4][b][e % 4];
-            h[e] = (ET)p;
-            l[e] = (ET)(p - (float)h[e]);
+        if (edge && rows > (int32_t)a.group.d) {
+          asm volatile("" ::: "memory");  // (the stage is not read where it need not be)
+          if (holds_nonfinite<ET, DP>(lds)) {
+#pragma unroll 1
+            for (int i = 0; i < 32 * DP; i += 512) clear_nonfinite<ET, 16>(lds + i, 0, 64);
+            cleared = true;
           }
-          hi[b] = __builtin_bit_cast(V8, h);
-          lo[b] = __builtin_bit_cast(V8, l);
         }
+        u32x4 hi[NB], lo[NB];
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const int row = 4 * g + n / 4;
-          const int piece = 2 * d + ((n & 3) >> 1), within = 4 * (n & 1);
-          typedef __attribute__((address_space(3))) s16x4* lds4;
-          const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds4)(lds + row * DP + 8 * (piece ^ swizzle4<DP>(row)) + within));
-          const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds4)(lds + (row + 16) * DP + 8 * (piece ^ swizzle4<DP>(row + 16)) + within));
-          const V8 f = __builtin_bit_cast(
-              V8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            o[d][b] = mfma16<ET>(f, hi[b], o[d][b]);
-            o[d][b] = mfma16<ET>(f, lo[b], o[d][b]);
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = x[2 * u + e / 2][b][e % 2 * 2], p1 = x[2 * u + e / 2][b][e % 2 * 2 + 1];
+            hi[b][e] = pack2<ET>(p0, p1);
+            lo[b][e] = pack2<ET>(p0 - low_half<ET>(hi[b][e]), p1 - high_half<ET>(hi[b][e]));
           }
+        // Reads of eight blocks of columns, then their products: each half of the weights in turn, so
+        // that no product waits for the one before.
+        constexpr int kColumns = DB < 8 ? DB : 8;
+#pragma unroll
+        for (int d0 = 0; d0 < DB; d0 += kColumns) {
+          V8 f[kColumns];
+#pragma unroll
+          for (int d = 0; d < kColumns; ++d) {
+            const int row = 4 * g + n / 4;
+            const int piece = 2 * (d0 + d) + ((n & 3) >> 1), within = 4 * (n & 1);
+            typedef __attribute__((address_space(3))) s16x4* lds4;
+            const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds4)(lds + row * DP + 8 * (piece ^ swizzle4<DP>(row)) + within));
+            const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds4)(lds + (row + 16) * DP + 8 * (piece ^ swizzle4<DP>(row + 16)) + within));
+            f[d] = __builtin_bit_cast(
+                V8, __builtin_shufflevector(first, second, 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int d = 0; d < kColumns; ++d)
+              o[d0 + d][b] = mfma16<ET>(f[d], __builtin_bit_cast(V8, hi[b]), o[d0 + d][b]);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int d = 0; d < kColumns; ++d)
+              o[d0 + d][b] = mfma16<ET>(f[d], __builtin_bit_cast(V8, lo[b]), o[d0 + d][b]);
         }
         asm volatile("" ::: "memory");
       }
     };
 
-    // The loads of the stage after are in flight while one is worked on.
-    L4 k0, v0, k1, v1;
-    load(jb, k0, v0);
-    for (int32_t j = jb; j < je; j += 2) {
-      if (j + 1 < je) load(j + 1, k1, v1);
-      __builtin_amdgcn_sched_barrier(0);
-      turn(j, k0, v0);
-      if (j + 1 >= je) break;
-      if (j + 2 < je) load(j + 2, k0, v0);
-      __builtin_amdgcn_sched_barrier(0);
-      turn(j + 1, k1, v1);
-    }
+    // Each block's registers take the next stage's codes as soon as they are converted.
+    find(jb);
+#pragma unroll
+    for (int t = 0; t < KT; ++t) load(a.k, a.k_scales, k, t);
+#pragma unroll
+    for (int t = 0; t < KT; ++t) load(a.v, a.v_scales, v, t);
+    for (int32_t j = jb; j < je - 1; ++j) turn(j, std::true_type{});
+    turn(je - 1, std::false_type{});
 
     float sum[NB];
     bool restore = cleared;
@@ -362,15 +459,18 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
   clear_tail(a, worker, grid);
 }
 
-template <typename ET, int DP, int NB>
+template <typename ET, int DP, int NB, bool EVEN>
 __global__ void __launch_bounds__(64, DP == 256 || NB == 2 ? 1 : 2) token4_kernel(AttnArgs a) {
   __shared__ __align__(16) uint16_t lds[32 * DP];
-  token4_work<ET, DP, NB>(a, blockIdx.x, lds);
+  token4_work<ET, DP, NB, EVEN>(a, blockIdx.x, lds);
 }
 
 template <typename ET, int DP>
 hipError_t launch_token4(const AttnArgs& a, hipStream_t s) {
-  const auto kern = a.skip_rows <= 16 ? token4_kernel<ET, DP, 1> : token4_kernel<ET, DP, 2>;
+  const bool even = a.page.d % 16 == 0;
+  const auto kern = a.skip_rows <= 16
+                        ? even ? token4_kernel<ET, DP, 1, true> : token4_kernel<ET, DP, 1, false>
+                        : even ? token4_kernel<ET, DP, 2, true> : token4_kernel<ET, DP, 2, false>;
   hipLaunchKernelGGL(kern, dim3((unsigned)token4_workers(DP)), dim3(64), 0, s, a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_token_join<ET, DP, (uint32_t)token4_workers(DP)>(a, s);

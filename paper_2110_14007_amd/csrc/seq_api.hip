@@ -248,8 +248,9 @@ tod_status check_cache4(const tod_cache4* c) {
   if (c->struct_size != sizeof(tod_cache4))
     return invalid("tod_cache4.struct_size does not match this library");
   if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return invalid("null pointer");
-  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16))
-    return invalid("codes must be 16-byte aligned");
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scales, 16) ||
+      !aligned(c->v_scales, 16))
+    return invalid("codes and scales must be 16-byte aligned");
   return TOD_OK;
 }
 

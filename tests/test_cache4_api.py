@@ -25,7 +25,7 @@ INVALID, WORKSPACE, UNSUPPORTED = 1, 3, 4
 
 def cache(tod, **kw):
     f = dict(struct_size=ctypes.sizeof(tod.tod_cache4), page_rows=16, n_pages=9, k_codes=at(),
-             v_codes=at(), k_scales=at(1), v_scales=at(3))
+             v_codes=at(), k_scales=at(), v_scales=at())
     f.update(kw)
     c = tod.tod_cache4()
     for name, v in f.items():
@@ -108,6 +108,7 @@ def test_append_pages_refused(tod, kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(struct_size=8), INVALID), (dict(k_codes=None), INVALID), (dict(v_codes=None), INVALID),
     (dict(k_scales=None), INVALID), (dict(v_scales=None), INVALID), (dict(k_codes=at(8)), INVALID),
+    (dict(k_scales=at(4)), INVALID), (dict(v_scales=at(1)), INVALID),
     (dict(n_pages=0), INVALID), (dict(page_rows=0), INVALID), (dict(page_rows=65537), INVALID),
     (dict(n_pages=1 << 30), UNSUPPORTED),
 ])
