@@ -50,7 +50,7 @@ __device__ __forceinline__ int32_t token_stages(const AttnArgs& a, int32_t s) {
   return s < a.n_seq ? token_stages<KEYS>(a, seq_of<true>(a, s)) : 0;
 }
 
-// Of `all` stages worker w of `grid` (a power of two) has those from share(w) on; where there are
+// Of `all` stages worker w of `grid` has those from share(w) on (all w: below 2^63); where there are
 // fewer stages than workers, one each.
 __device__ __forceinline__ int64_t share(int64_t w, int64_t all, const uint32_t grid) {
   return all < grid ? w : (all * w) / grid;

@@ -76,7 +76,7 @@ __device__ __forceinline__ float high_half(uint32_t w) {
 }
 
 template <int DP>
-constexpr int token4_tiles() { return DP == 256 ? 2 : 4; }  // blocks of 16 keys of a stage
+constexpr int token4_tiles() { return DP == 64 ? 4 : 2; }  // blocks of 16 keys of a stage
 template <int DP>
 constexpr int token4_keys() { return 16 * token4_tiles<DP>(); }
 
@@ -358,9 +358,9 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
             hi[b][e] = pack2<ET>(p0, p1);
             lo[b][e] = pack2<ET>(p0 - low_half<ET>(hi[b][e]), p1 - high_half<ET>(hi[b][e]));
           }
-        // Reads of eight blocks of columns, then their products: each half of the weights in turn, so
+        // Reads of four blocks of columns, then their products: each half of the weights in turn, so
         // that no product waits for the one before.
-        constexpr int kColumns = DB < 8 ? DB : 8;
+        constexpr int kColumns = 4;
 #pragma unroll
         for (int d0 = 0; d0 < DB; d0 += kColumns) {
           V8 f[kColumns];
@@ -459,8 +459,12 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
   clear_tail(a, worker, grid);
 }
 
+// Waves on a SIMD, by the registers that they need.
+template <int DP, int NB>
+constexpr int token4_waves() { return DP == 256 ? NB == 1 ? 2 : 1 : NB == 1 ? 3 : 2; }
+
 template <typename ET, int DP, int NB, bool EVEN>
-__global__ void __launch_bounds__(64, DP == 256 || NB == 2 ? 1 : 2) token4_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(64, (token4_waves<DP, NB>())) token4_kernel(AttnArgs a) {
   __shared__ __align__(16) uint16_t lds[32 * DP];
   token4_work<ET, DP, NB, EVEN>(a, blockIdx.x, lds);
 }

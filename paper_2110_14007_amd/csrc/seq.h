@@ -108,8 +108,8 @@ constexpr int kTokenMaxRows = 32;
 // TB/s with four a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
 constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
-// Over a 4-bit cache: two waves on each of 1,024 SIMDs, one for more than 128 elements.
-constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 1024 : 2048; }
+// Over a 4-bit cache: three waves on each of 1,024 SIMDs, two for more than 128 elements.
+constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 2048 : 3072; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);
