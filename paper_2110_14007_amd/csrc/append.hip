@@ -6,8 +6,8 @@
 // head are a pair (x, y) that turns by the angle pos * rate_i:
 //   x' = x cos - y sin,  y' = x sin + y cos.
 // The angle of a far position has to be right to a small part of a turn, so
-// that it is formed in 64 bits, where the product of a 32-bit position and a
-// 24-bit rate is exact below 2^53, and so are its cosine and sine.
+// that it is formed and reduced in 64 bits, where the product of a 32-bit
+// position and a 24-bit rate is exact below 2^53.
 //
 // 4-bit rows.  Of 32 elements with the largest magnitude a, the scale 2^e is
 // the smallest with a <= 7 2^e: then the largest error is 2^e, at 7 and
@@ -45,38 +45,66 @@ __device__ __forceinline__ float element(const u32x4& w, int i) {
   return (float)__builtin_bit_cast(ET, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
 }
 
-// Eight elements from e0 on of a head at p, rotated, in the arithmetic of T.  Pairs that are
-// halves apart by a multiple of 8 elements lie in two loads of 16 bytes (WIDE), others are read one by
-// one.
-template <typename ET, typename T, bool PAIRS, bool WIDE, typename Angle>
-__device__ __forceinline__ void rotate(T (&x)[8], const uint16_t* p, int e0, int rotary,
-                                       const Angle* turn) {
-  const u32x4 w = *(const u32x4*)(p + e0);
+// How a head's pairs lie: neighbours, halves apart by a multiple of 8 elements (a piece's partners
+// are a piece too), or halves apart otherwise.
+enum class Pairs { kNeighbours, kPieces, kOdd };
+
+// What the rotation of the eight elements from e0 on needs of the row at p.  What there is nothing to
+// load for, is loaded from the row's start: there is no branch around the loads.
+template <Pairs PAIRS>
+struct Piece {
+  u32x4 own, other;  // other: the partners, for kPieces
+};
+
+template <Pairs PAIRS>
+__device__ __forceinline__ Piece<PAIRS> load_piece(const uint16_t* p, int e0, int rotary) {
+  Piece<PAIRS> w;
+  w.own = *(const u32x4*)(p + e0);
+  if constexpr (PAIRS == Pairs::kPieces) {
+    const int half = rotary / 2;
+    w.other = *(const u32x4*)(p + (e0 >= rotary ? 0 : e0 < half ? e0 + half : e0 - half));
+  }
+  return w;
+}
+
+// Where the angle of pair m lies in LDS: the threads of a row read angles that are 8 (4) pairs apart.
+template <Pairs PAIRS>
+__device__ __forceinline__ int place_of(int m, int half) {
+  if constexpr (PAIRS == Pairs::kNeighbours)
+    return m % 4 * ((half + 3) / 4) + m / 4;
+  else if constexpr (PAIRS == Pairs::kPieces)
+    return m % 8 * (half / 8) + m / 8;
+  else
+    return m;
+}
+
+// The eight elements from e0 on, rotated, in the arithmetic of T.
+template <typename ET, typename T, Pairs PAIRS, typename Angle>
+__device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const uint16_t* p, int e0,
+                                       int rotary, const Angle* turn) {
+  const int half = rotary / 2;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (T)element<ET>(w, i);
+  for (int i = 0; i < 8; ++i) x[i] = (T)element<ET>(w.own, i);
   if (e0 >= rotary) return;
-  if constexpr (PAIRS) {
+  if constexpr (PAIRS == Pairs::kNeighbours) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       if (e0 + i >= rotary) break;
-      const Angle t = turn[(e0 + i) / 2];
+      const Angle t = turn[i / 2 * ((half + 3) / 4) + e0 / 8];
       const T a = x[i], b = x[i + 1];
       x[i] = a * (T)t.x - b * (T)t.y;
       x[i + 1] = a * (T)t.y + b * (T)t.x;
     }
-  } else if constexpr (WIDE) {
-    const int half = rotary / 2;
+  } else if constexpr (PAIRS == Pairs::kPieces) {
     const bool first = e0 < half;
-    const u32x4 v = *(const u32x4*)(p + (first ? e0 + half : e0 - half));
-    const Angle* const at = turn + (first ? e0 : e0 - half);
+    const Angle* const at = turn + (first ? e0 : e0 - half) / 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const Angle t = at[i];
-      const T other = (T)element<ET>(v, i), s = (T)t.y;
+      const Angle t = at[i * (half / 8)];
+      const T other = (T)element<ET>(w.other, i), s = (T)t.y;
       x[i] = x[i] * (T)t.x + other * (first ? -s : s);
     }
   } else {
-    const int half = rotary / 2;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int e = e0 + i;
@@ -154,61 +182,173 @@ __device__ __forceinline__ uint32_t encode(const double (&x)[8], uint32_t* scale
   return codes;
 }
 
-// A workgroup takes a token at a time: its angles' cosines and sines go to LDS, then each thread
-// takes 16-byte pieces of the query heads, the keys and the values.
-template <typename ET, bool FOUR, bool PAIRS, bool WIDE>
+// The same for elements as they are: the conversion to codes rounds as code_of does, from a 16-bit
+// element straight.
+template <typename ET>
+__device__ __forceinline__ uint32_t encode16(const u32x4& w, uint32_t* scale) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  constexpr uint32_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  int top = max((int)m[0], (int)m[1]);  // magnitudes compare as their bits
+  top = max(top, __shfl_xor(top, 1, 64));
+  top = max(top, __shfl_xor(top, 2, 64));
+  if (top >= (int)kInf) {
+    *scale = 255;
+    return 0;
+  }
+  const int e = block_exponent<ET>((double)(float)__builtin_bit_cast(ET, (uint16_t)top));
+  *scale = (uint32_t)(e + 127);
+  const float by = scale_of(*scale);
+  uint32_t codes = 0;
+  codes = two_codes<ET, 0>(codes, w[0], by);
+  codes = two_codes<ET, 1>(codes, w[1], by);
+  codes = two_codes<ET, 2>(codes, w[2], by);
+  return two_codes<ET, 3>(codes, w[3], by);
+}
+
+// Cosine and sine of an angle of fewer than 2^31 radians: the angle less the nearest multiple n of a
+// quarter turn, in two parts (the first difference is exact, for its terms are multiples of 2^-52 and
+// it is small), then the Taylor series to the terms that a T holds, and the quarter's exchange.
+template <typename T>
+__device__ __forceinline__ void turn_by(double angle, T* cosine, T* sine) {
+  constexpr double kQuarter = 0x1.921fb54442d18p+0, kRest = 0x1.1a62633145c07p-54;  // pi / 2
+  if (fabs(angle) >= 0x1p31) {  // (a NaN too, below)
+    double s, c;
+    sincos(angle, &s, &c);
+    *cosine = (T)c;
+    *sine = (T)s;
+    return;
+  }
+  const double n = rint(angle * 0.63661977236758134308);
+  const T r = (T)fma(-n, kRest, fma(-n, kQuarter, angle));
+  const T x = r * r;
+  T s, c;
+  if constexpr (sizeof(T) == 8) {
+    s = 1.0 / 355687428096000.0;
+    s = fma(s, x, -1.0 / 1307674368000.0);
+    s = fma(s, x, 1.0 / 6227020800.0);
+    s = fma(s, x, -1.0 / 39916800.0);
+    s = fma(s, x, 1.0 / 362880.0);
+    s = fma(s, x, -1.0 / 5040.0);
+    s = fma(s, x, 1.0 / 120.0);
+    s = fma(s, x, -1.0 / 6.0);
+    c = -1.0 / 6402373705728000.0;
+    c = fma(c, x, 1.0 / 20922789888000.0);
+    c = fma(c, x, -1.0 / 87178291200.0);
+    c = fma(c, x, 1.0 / 479001600.0);
+    c = fma(c, x, -1.0 / 3628800.0);
+    c = fma(c, x, 1.0 / 40320.0);
+    c = fma(c, x, -1.0 / 720.0);
+    c = fma(c, x, 1.0 / 24.0);
+    c = fma(c, x, -0.5);
+    s = fma(s * x, r, r);
+    c = fma(c, x, 1.0);
+  } else {
+    s = 1.0f / 362880.0f;
+    s = fmaf(s, x, -1.0f / 5040.0f);
+    s = fmaf(s, x, 1.0f / 120.0f);
+    s = fmaf(s, x, -1.0f / 6.0f);
+    c = -1.0f / 3628800.0f;
+    c = fmaf(c, x, 1.0f / 40320.0f);
+    c = fmaf(c, x, -1.0f / 720.0f);
+    c = fmaf(c, x, 1.0f / 24.0f);
+    c = fmaf(c, x, -0.5f);
+    s = fmaf(s * x, r, r);
+    c = fmaf(c, x, 1.0f);
+  }
+  const int q = (int)n;
+  const T p = q & 1 ? s : c, t = q & 1 ? c : s;
+  *cosine = (q + 1) & 2 ? -p : p;
+  *sine = q & 2 ? -t : t;
+}
+
+enum class Rows { kQueries, kKeys, kValues };
+
+// A workgroup takes TOKENS tokens at a time: their angles' cosines and sines go to LDS, then each
+// thread takes one 16-byte piece of every so many of their rows, several rows' loads at once.
+template <typename ET, bool FOUR, Pairs PAIRS, int TOKENS>
 __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
-  __shared__ double2 turn[kMostAngles];
+  using T = typename std::conditional<FOUR, double, float>::type;  // of rotated keys
+  using Angle = typename std::conditional<FOUR, double2, float2>::type;
+  __shared__ Angle turn[TOKENS][kMostAngles];
   const int tid = threadIdx.x;
   const int32_t per_row = (int32_t)a.per_row.d, half = a.rotary / 2;
-  const int32_t hq = a.heads, hk = a.kv_heads, pieces = (hq + 2 * hk) * per_row;
-  for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
-    const int64_t slot = a.slot[t];
-    const double pos = (double)a.pos[t];
-    __syncthreads();  // the token before is done with the angles
-    for (int i = tid; i < half; i += kThreads) {
-      double2 w;
-      sincos(pos * (double)a.rates[i], &w.y, &w.x);
-      turn[i] = w;
+  const int32_t step = (int32_t)a.step;  // rows of a pass; threads past them have none
+  const int32_t r0 = (int32_t)div_by((uint32_t)tid, a.per_row), c = tid - r0 * per_row;
+
+  for (int64_t t0 = (int64_t)blockIdx.x * TOKENS; t0 < a.tokens; t0 += (int64_t)gridDim.x * TOKENS) {
+    const int32_t count = (int32_t)min((int64_t)TOKENS, a.tokens - t0);
+    __syncthreads();  // the tokens before are done with the angles
+    for (int i = tid; i < count * half; i += kThreads) {
+      const int32_t k = (int32_t)div_by((uint32_t)i, a.angles), m = i - k * half;
+      Angle& to = turn[k][place_of<PAIRS>(m, half)];
+      turn_by<T>((double)a.pos[t0 + k] * (double)a.rates[m], &to.x, &to.y);
     }
     __syncthreads();
-    const bool kept = slot >= 0 && slot < a.slots;
-    const uint32_t page = kept ? div_by((uint32_t)slot, a.page) : 0u;
-    const uint32_t row = kept ? (uint32_t)slot - page * a.page.d : 0u;
-    for (int32_t p = tid; p < pieces; p += kThreads) {
-      const int32_t h = (int32_t)div_by((uint32_t)p, a.per_row), c = p - h * per_row;
-      if (h < hq) {
-        float x[8];
-        rotate<ET, float, PAIRS, WIDE>(x, (const uint16_t*)a.q + t * a.q_row + h * a.q_head, 8 * c,
-                                       a.rotary, turn);
-        ((u32x4*)a.q_out)[(t * hq + h) * per_row + c] = rounded<ET>(x);
-        continue;
-      }
-      if (!kept) continue;
-      const bool isk = h < hq + hk;
-      const int32_t kh = h - hq - (isk ? 0 : hk);
-      const uint16_t* const from = isk ? (const uint16_t*)a.k + t * a.k_row + kh * a.k_head
-                                       : (const uint16_t*)a.v + t * a.v_row + kh * a.v_head;
-      const int64_t to = (((int64_t)page * hk + kh) * a.page.d + row) * per_row + c;
-      if constexpr (FOUR) {
-        double x[8];
-        rotate<ET, double, PAIRS, WIDE>(x, from, 8 * c, isk ? a.rotary : 0, turn);
-        uint32_t scale;
-        const uint32_t codes = encode<ET>(x, &scale);
-        ((uint32_t*)(isk ? a.k_pages : a.v_pages))[to] = codes;
-        if (c % 4 == 0) (isk ? a.k_scales : a.v_scales)[to / 4] = (uint8_t)scale;
-      } else {
-        u32x4 w;
-        if (isk) {
-          float x[8];
-          rotate<ET, float, PAIRS, WIDE>(x, from, 8 * c, a.rotary, turn);
-          w = rounded<ET>(x);
-        } else {
-          w = *(const u32x4*)(from + 8 * c);
+
+    auto pass = [&](auto KIND, const FastDiv& heads, const void* rows, int64_t token_stride,
+                    int64_t head_stride) __attribute__((always_inline)) {
+      constexpr Rows kind = decltype(KIND)::value;
+      constexpr Pairs pairs = kind == Rows::kValues ? Pairs::kOdd : PAIRS;  // (values have no partners)
+      constexpr int kAhead = FOUR && kind == Rows::kKeys ? 2 : 4;
+      const int32_t n = r0 < step ? count * (int32_t)heads.d : 0;
+      for (int32_t r = r0; r < n; r += kAhead * step) {
+        const uint16_t* from[kAhead];
+        Piece<pairs> w[kAhead];
+        int64_t slot[kAhead];
+        int32_t tok[kAhead], head[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int32_t at = min(r + i * step, n - 1);
+          tok[i] = (int32_t)div_by((uint32_t)at, heads);
+          head[i] = at - tok[i] * (int32_t)heads.d;
+          from[i] = (const uint16_t*)rows + (t0 + tok[i]) * token_stride + head[i] * head_stride;
+          if constexpr (kind != Rows::kQueries) slot[i] = a.slot[t0 + tok[i]];
+          w[i] = load_piece<pairs>(from[i], 8 * c, a.rotary);
         }
-        ((u32x4*)(isk ? a.k_pages : a.v_pages))[to] = w;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (r + i * step >= n) break;
+          const Angle* const angles = turn[tok[i]];
+          if constexpr (kind == Rows::kQueries) {
+            float x[8];
+            rotate<ET, float, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+            ((u32x4*)a.q_out)[((t0 + tok[i]) * a.heads + head[i]) * per_row + c] = rounded<ET>(x);
+          } else {
+            if (slot[i] < 0 || slot[i] >= a.slots) continue;
+            const uint32_t page = div_by((uint32_t)slot[i], a.page);
+            const uint32_t row = (uint32_t)slot[i] - page * a.page.d;
+            const int64_t to =
+                (((int64_t)page * a.kv_heads + head[i]) * a.page.d + row) * per_row + c;
+            void* const pages = kind == Rows::kKeys ? a.k_pages : a.v_pages;
+            if constexpr (FOUR) {
+              uint32_t scale;
+              if constexpr (kind == Rows::kKeys) {
+                T x[8];
+                rotate<ET, T, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+                ((uint32_t*)pages)[to] = encode<ET>(x, &scale);
+              } else {
+                ((uint32_t*)pages)[to] = encode16<ET>(w[i].own, &scale);
+              }
+              if (c % 4 == 0)
+                (kind == Rows::kKeys ? a.k_scales : a.v_scales)[to / 4] = (uint8_t)scale;
+            } else if constexpr (kind == Rows::kKeys) {
+              T x[8];
+              rotate<ET, T, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+              ((u32x4*)pages)[to] = rounded<ET>(x);
+            } else {
+              ((u32x4*)pages)[to] = w[i].own;
+            }
+          }
+        }
       }
-    }
+    };
+    pass(std::integral_constant<Rows, Rows::kQueries>{}, a.q_heads, a.q, a.q_row, a.q_head);
+    pass(std::integral_constant<Rows, Rows::kKeys>{}, a.k_heads, a.k, a.k_row, a.k_head);
+    pass(std::integral_constant<Rows, Rows::kValues>{}, a.k_heads, a.v, a.v_row, a.v_head);
   }
 }
 
@@ -234,15 +374,28 @@ __global__ void __launch_bounds__(kThreads) read4_kernel(Read4Args a) {
   ((u32x4*)a.v_out)[to] = v;
 }
 
-template <typename ET, bool FOUR>
+template <typename ET, bool FOUR, Pairs PAIRS>
 hipError_t launch_append(const AppendArgs& a, hipStream_t s) {
+  constexpr int kTokens = 4;
   const int64_t most = 1 << 20;
-  const dim3 grid((unsigned)(a.tokens < most ? a.tokens : most));
-  const auto kern = a.interleaved               ? append_kernel<ET, FOUR, true, true>
-                    : a.rotary / 2 % 8 == 0 ? append_kernel<ET, FOUR, false, true>
-                                                : append_kernel<ET, FOUR, false, false>;
-  hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, s, a);
+  // One token a workgroup while there are few of them.
+  const bool few = a.tokens <= 2048;
+  const int64_t groups = few ? a.tokens : (a.tokens + kTokens - 1) / kTokens;
+  hipLaunchKernelGGL((few ? append_kernel<ET, FOUR, PAIRS, 1> : append_kernel<ET, FOUR, PAIRS, kTokens>),
+                     dim3((unsigned)(groups < most ? groups : most)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
+}
+
+template <typename ET, bool FOUR>
+hipError_t launch_append(const AppendArgs& given, hipStream_t s) {
+  AppendArgs a = given;
+  a.step = kThreads / a.per_row.d;
+  a.q_heads = fast_div((uint32_t)a.heads);
+  a.k_heads = fast_div((uint32_t)a.kv_heads);
+  a.angles = fast_div((uint32_t)(a.rotary > 2 ? a.rotary / 2 : 1));
+  if (a.interleaved) return launch_append<ET, FOUR, Pairs::kNeighbours>(a, s);
+  if (a.rotary % 16 == 0) return launch_append<ET, FOUR, Pairs::kPieces>(a, s);
+  return launch_append<ET, FOUR, Pairs::kOdd>(a, s);
 }
 
 }  // namespace

@@ -59,6 +59,8 @@ struct AppendArgs {
   uint8_t *k_scales, *v_scales;
   int64_t tokens, slots;  // slots: n_pages * page
   FastDiv page, per_row;  // 8-element pieces of a head's row
+  FastDiv q_heads, k_heads, angles;  // heads; pairs of a head
+  uint32_t step;                     // rows of a pass of a workgroup
   int32_t heads, kv_heads, rotary, interleaved;
 };
 

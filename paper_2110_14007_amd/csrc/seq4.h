@@ -33,4 +33,16 @@ __device__ __forceinline__ auto eight_values(uint32_t codes, float scale) {
                two_values<ET, 2>(codes, scale), two_values<ET, 3>(codes, scale)};
 }
 
+// Byte SEL of `codes` from two 16-bit elements over the scale: the nearest values, ties to the even
+// code, beyond 6 to 6.
+template <typename ET, int SEL>
+__device__ __forceinline__ uint32_t two_codes(uint32_t codes, uint32_t pair, float scale) {
+  typedef ET e2 __attribute__((ext_vector_type(2)));
+  if constexpr (std::is_same<ET, _Float16>::value)
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(codes, __builtin_bit_cast(e2, pair), scale, SEL);
+  else
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(e2, pair), scale,
+                                                     SEL);
+}
+
 }  // namespace tod
