@@ -13,8 +13,9 @@
 // the smallest with a <= 7 2^e: then the largest error is 2^e, at 7 and
 // between 4 and 6 alike.  e stays in [-23, 13] (fp16) or [-125, 125] (bf16), so
 // that every value that a code and a scale stand for is a number of the type.
-// Rotated keys are scaled and rounded in 64 bits: an element next to the border
-// of two codes gets the one that the formula gives.
+// Keys are rotated in 64 bits and compared with the borders of scales and codes
+// as what they are there: an element next to a border gets the code that the
+// formula gives.
 #include "seq.h"
 
 #include "seq4.h"
@@ -40,9 +41,14 @@ struct Exponents<__bf16> {
   static constexpr int lo = -125, hi = 125;
 };
 
-template <typename ET>
-__device__ __forceinline__ float element(const u32x4& w, int i) {
-  return (float)__builtin_bit_cast(ET, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
+template <typename ET, typename T>
+__device__ __forceinline__ T number(uint16_t u) {
+  const float f = (float)__builtin_bit_cast(ET, u);
+  return sizeof(T) == 8 ? (T)(0.5f * f) : (T)f;
+}
+template <typename ET, typename T>
+__device__ __forceinline__ T element(const u32x4& w, int i) {
+  return number<ET, T>((uint16_t)(w[i / 2] >> (16 * (i % 2))));
 }
 
 // How a head's pairs lie: neighbours, halves apart by a multiple of 8 elements (a piece's partners
@@ -78,13 +84,13 @@ __device__ __forceinline__ int place_of(int m, int half) {
     return m;
 }
 
-// The eight elements from e0 on, rotated, in the arithmetic of T.
+// The eight elements from e0 on, rotated, in the arithmetic of T (double: halved, see encode).
 template <typename ET, typename T, Pairs PAIRS, typename Angle>
 __device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const uint16_t* p, int e0,
                                        int rotary, const Angle* turn) {
   const int half = rotary / 2;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (T)element<ET>(w.own, i);
+  for (int i = 0; i < 8; ++i) x[i] = element<ET, T>(w.own, i);
   if (e0 >= rotary) return;
   if constexpr (PAIRS == Pairs::kNeighbours) {
 #pragma unroll
@@ -101,7 +107,7 @@ __device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const u
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const Angle t = at[i * (half / 8)];
-      const T other = (T)element<ET>(w.other, i), s = (T)t.y;
+      const T other = element<ET, T>(w.other, i), s = (T)t.y;
       x[i] = x[i] * (T)t.x + other * (first ? -s : s);
     }
   } else {
@@ -111,7 +117,7 @@ __device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const u
       if (e >= rotary) break;
       const bool first = e < half;
       const Angle t = turn[first ? e : e - half];
-      const T other = (T)(float)__builtin_bit_cast(ET, p[first ? e + half : e - half]);
+      const T other = number<ET, T>(p[first ? e + half : e - half]);
       const T s = (T)t.y;
       x[i] = x[i] * (T)t.x + other * (first ? -s : s);
     }
@@ -130,60 +136,57 @@ __device__ __forceinline__ u32x4 rounded(const T (&x)[8]) {
   return w;
 }
 
-// Exponent of the scale of a block whose largest magnitude is a (finite): from a = f 2^E with
-// 1 <= f < 2, a <= 7 2^e = 1.75 2^(e + 2) holds from e = E - 2 on if f <= 1.75, else from E - 1.
+// y as a float on the same side of every float that y is: what y rounds to, or its neighbour towards y.
+// Borders of codes and of scales are floats, so that comparisons with them come out as y's do.
+__device__ __forceinline__ float beside(double y) {
+  const float f = (float)y;
+  const uint32_t u = __float_as_uint(f);
+  const double back = (double)f;
+  return __uint_as_float(back == y ? u : fabs(y) > fabs(back) ? u + 1 : u - 1);
+}
+
+// Exponent of the scale of a block whose largest magnitude is a (finite), from a's bits: from
+// a = f 2^E with 1 <= f < 2, a <= 7 2^e = 1.75 2^(e + 2) holds from e = E - 2 on if f <= 1.75, else
+// from E - 1.  (Below the normal numbers the least e is right.)
 template <typename ET>
-__device__ __forceinline__ int block_exponent(double a) {
-  const uint64_t u = (uint64_t)__double_as_longlong(a);
-  const int e = (int)(u >> 52) - 1025 + ((u & 0xfffffffffffffull) > 0xc000000000000ull ? 1 : 0);
+__device__ __forceinline__ int block_exponent(uint32_t a, int more) {
+  const int e = (int)(a >> 23) - 129 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0) + more;
   return min(max(e, Exponents<ET>::lo), Exponents<ET>::hi);
 }
 
-__device__ __forceinline__ double power2(int e) {
-  return __longlong_as_double((long long)(e + 1023) << 52);
-}
-
-// Code of x, in units of the scale: below 2 in steps of 1/2, below 4 of 1, from there of 2 up to 6,
-// ties to the even code.
-__device__ __forceinline__ uint32_t code_of(double x) {
-  const double m = fabs(x);
-  const double n = m < 2.0 ? rint(m + m) : m < 4.0 ? rint(m) + 2.0 : rint(0.5 * m) + 4.0;
-  return (uint32_t)fmin(n, 7.0) | (x < 0.0 ? 8u : 0u);
-}
-
 // Maximum over the four lanes that hold a block.
-template <typename T>
-__device__ __forceinline__ T over_block(T v) {
-  v = fmax(v, __shfl_xor(v, 1, 64));
-  return fmax(v, __shfl_xor(v, 2, 64));
+__device__ __forceinline__ uint32_t over_block(uint32_t v) {
+  v = max(v, (uint32_t)__shfl_xor((int)v, 1, 64));
+  return max(v, (uint32_t)__shfl_xor((int)v, 2, 64));
 }
 
 // Codes of a lane's eight elements of a block, and the block's scale byte: 255 (and the codes 0)
-// where an element is not finite.  Four lanes in a row hold a block.
+// where an element is not finite.  Four lanes in a row hold a block.  The elements come halved: a
+// rotated one may be larger than its type's numbers are.
 template <typename ET>
 __device__ __forceinline__ uint32_t encode(const double (&x)[8], uint32_t* scale) {
-  double top = 0.0;
+  float f[8];
+  uint32_t top = 0;  // magnitudes compare as their bits
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const double m = fabs(x[i]);
-    top = fmax(top, m <= 1.7e308 ? m : HUGE_VAL);  // (a NaN too)
+    f[i] = beside(x[i]);
+    top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
   }
   top = over_block(top);
-  if (!(top <= 1.7e308)) {
+  if (top >= 0x7f800000u) {
     *scale = 255;
     return 0;
   }
-  const int e = block_exponent<ET>(top);
-  *scale = (uint32_t)(e + 127);
-  const double by = power2(-e);
+  *scale = (uint32_t)(block_exponent<ET>(top, 1) + 127);
+  const float by = scale_of(*scale - 1);
   uint32_t codes = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) codes |= code_of(x[i] * by) << (4 * i);
-  return codes;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], by, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], by, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], by, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], by, 3);
 }
 
-// The same for elements as they are: the conversion to codes rounds as code_of does, from a 16-bit
-// element straight.
+// The same for elements as they are.
 template <typename ET>
 __device__ __forceinline__ uint32_t encode16(const u32x4& w, uint32_t* scale) {
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -192,15 +195,13 @@ __device__ __forceinline__ uint32_t encode16(const u32x4& w, uint32_t* scale) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
-  int top = max((int)m[0], (int)m[1]);  // magnitudes compare as their bits
-  top = max(top, __shfl_xor(top, 1, 64));
-  top = max(top, __shfl_xor(top, 2, 64));
-  if (top >= (int)kInf) {
+  const uint32_t top = over_block(max((uint32_t)m[0], (uint32_t)m[1]));
+  if (top >= kInf) {
     *scale = 255;
     return 0;
   }
-  const int e = block_exponent<ET>((double)(float)__builtin_bit_cast(ET, (uint16_t)top));
-  *scale = (uint32_t)(e + 127);
+  const float a = (float)__builtin_bit_cast(ET, (uint16_t)top);
+  *scale = (uint32_t)(block_exponent<ET>(__float_as_uint(a), 0) + 127);
   const float by = scale_of(*scale);
   uint32_t codes = 0;
   codes = two_codes<ET, 0>(codes, w[0], by);
