@@ -43,8 +43,7 @@ struct Exponents<__bf16> {
 
 template <typename ET, typename T>
 __device__ __forceinline__ T number(uint16_t u) {
-  const float f = (float)__builtin_bit_cast(ET, u);
-  return sizeof(T) == 8 ? (T)(0.5f * f) : (T)f;
+  return (T)(float)__builtin_bit_cast(ET, u);
 }
 template <typename ET, typename T>
 __device__ __forceinline__ T element(const u32x4& w, int i) {
@@ -84,31 +83,41 @@ __device__ __forceinline__ int place_of(int m, int half) {
     return m;
 }
 
-// The eight elements from e0 on, rotated, in the arithmetic of T (double: halved, see encode).
+// The eight elements from e0 on, rotated, in the arithmetic of T.  `unit` is what the angles' cosines
+// and sines are scaled by.
 template <typename ET, typename T, Pairs PAIRS, typename Angle>
 __device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const uint16_t* p, int e0,
-                                       int rotary, const Angle* turn) {
+                                       int rotary, const Angle* turn, T unit) {
   const int half = rotary / 2;
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = element<ET, T>(w.own, i);
-  if (e0 >= rotary) return;
+  if (PAIRS == Pairs::kOdd || e0 >= rotary) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= unit;
+    if (e0 >= rotary) return;
+  }
   if constexpr (PAIRS == Pairs::kNeighbours) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      if (e0 + i >= rotary) break;
-      const Angle t = turn[i / 2 * ((half + 3) / 4) + e0 / 8];
-      const T a = x[i], b = x[i + 1];
-      x[i] = a * (T)t.x - b * (T)t.y;
-      x[i + 1] = a * (T)t.y + b * (T)t.x;
+      if (e0 + i < rotary) {
+        const Angle t = turn[i / 2 * ((half + 3) / 4) + e0 / 8];
+        const T a = x[i], b = x[i + 1];
+        x[i] = a * t.x - b * t.y;
+        x[i + 1] = a * t.y + b * t.x;
+      } else {
+        x[i] *= unit;
+        x[i + 1] *= unit;
+      }
     }
   } else if constexpr (PAIRS == Pairs::kPieces) {
     const bool first = e0 < half;
     const Angle* const at = turn + (first ? e0 : e0 - half) / 8;
+    // The first of a pair takes its partner's sine with the other sign: the partner's is changed.
+    const u32x4 other = w.other ^ (first ? 0x80008000u : 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const Angle t = at[i * (half / 8)];
-      const T other = element<ET, T>(w.other, i), s = (T)t.y;
-      x[i] = x[i] * (T)t.x + other * (first ? -s : s);
+      x[i] = x[i] * t.x + element<ET, T>(other, i) * t.y;
     }
   } else {
 #pragma unroll
@@ -118,20 +127,21 @@ __device__ __forceinline__ void rotate(T (&x)[8], const Piece<PAIRS>& w, const u
       const bool first = e < half;
       const Angle t = turn[first ? e : e - half];
       const T other = number<ET, T>(p[first ? e + half : e - half]);
-      const T s = (T)t.y;
-      x[i] = x[i] * (T)t.x + other * (first ? -s : s);
+      x[i] = element<ET, T>(w.own, i) * t.x + other * (first ? -t.y : t.y);
     }
   }
 }
 
-template <typename ET, typename T>
-__device__ __forceinline__ u32x4 rounded(const T (&x)[8]) {
+template <typename ET>
+__device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
+  typedef ET e2 __attribute__((ext_vector_type(2)));
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const ET a = (ET)(float)x[2 * i], b = (ET)(float)x[2 * i + 1];
-    w[i] = (uint32_t)__builtin_bit_cast(uint16_t, a) |
-           (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+    e2 v;
+    v[0] = (ET)x[2 * i];
+    v[1] = (ET)x[2 * i + 1];
+    w[i] = __builtin_bit_cast(uint32_t, v);
   }
   return w;
 }
@@ -269,12 +279,12 @@ __device__ __forceinline__ void turn_by(double angle, T* cosine, T* sine) {
 enum class Rows { kQueries, kKeys, kValues };
 
 // A workgroup takes TOKENS tokens at a time: their angles' cosines and sines go to LDS, then each
-// thread takes one 16-byte piece of every so many of their rows, several rows' loads at once.
+// thread takes one 16-byte piece of every so many of their rows, several rows' loads at once.  For a
+// 4-bit cache keys are rotated in 64 bits and halved (see encode).
 template <typename ET, bool FOUR, Pairs PAIRS, int TOKENS>
 __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
-  using T = typename std::conditional<FOUR, double, float>::type;  // of rotated keys
-  using Angle = typename std::conditional<FOUR, double2, float2>::type;
-  __shared__ Angle turn[TOKENS][kMostAngles];
+  __shared__ float2 turn[TOKENS][kMostAngles];
+  __shared__ double2 turn4[FOUR ? TOKENS : 1][kMostAngles];
   const int tid = threadIdx.x;
   const int32_t per_row = (int32_t)a.per_row.d, half = a.rotary / 2;
   const int32_t step = (int32_t)a.step;  // rows of a pass; threads past them have none
@@ -285,8 +295,18 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     __syncthreads();  // the tokens before are done with the angles
     for (int i = tid; i < count * half; i += kThreads) {
       const int32_t k = (int32_t)div_by((uint32_t)i, a.angles), m = i - k * half;
-      Angle& to = turn[k][place_of<PAIRS>(m, half)];
-      turn_by<T>((double)a.pos[t0 + k] * (double)a.rates[m], &to.x, &to.y);
+      const double angle = (double)a.pos[t0 + k] * (double)a.rates[m];
+      const int at = place_of<PAIRS>(m, half);
+      if constexpr (FOUR) {
+        double x, y;
+        turn_by<double>(angle, &x, &y);
+        turn[k][at] = {(float)x, (float)y};
+        turn4[k][at] = {0.5 * x, 0.5 * y};
+      } else {
+        float x, y;
+        turn_by<float>(angle, &x, &y);
+        turn[k][at] = {x, y};
+      }
     }
     __syncthreads();
 
@@ -313,10 +333,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
           if (r + i * step >= n) break;
-          const Angle* const angles = turn[tok[i]];
           if constexpr (kind == Rows::kQueries) {
             float x[8];
-            rotate<ET, float, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+            rotate<ET, float, pairs>(x, w[i], from[i], 8 * c, a.rotary, turn[tok[i]], 1.0f);
             ((u32x4*)a.q_out)[((t0 + tok[i]) * a.heads + head[i]) * per_row + c] = rounded<ET>(x);
           } else {
             if (slot[i] < 0 || slot[i] >= a.slots) continue;
@@ -328,8 +347,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
             if constexpr (FOUR) {
               uint32_t scale;
               if constexpr (kind == Rows::kKeys) {
-                T x[8];
-                rotate<ET, T, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+                double x[8];
+                rotate<ET, double, pairs>(x, w[i], from[i], 8 * c, a.rotary, turn4[tok[i]], 0.5);
                 ((uint32_t*)pages)[to] = encode<ET>(x, &scale);
               } else {
                 ((uint32_t*)pages)[to] = encode16<ET>(w[i].own, &scale);
@@ -337,8 +356,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
               if (c % 4 == 0)
                 (kind == Rows::kKeys ? a.k_scales : a.v_scales)[to / 4] = (uint8_t)scale;
             } else if constexpr (kind == Rows::kKeys) {
-              T x[8];
-              rotate<ET, T, pairs>(x, w[i], from[i], 8 * c, a.rotary, angles);
+              float x[8];
+              rotate<ET, float, pairs>(x, w[i], from[i], 8 * c, a.rotary, turn[tok[i]], 1.0f);
               ((u32x4*)pages)[to] = rounded<ET>(x);
             } else {
               ((u32x4*)pages)[to] = w[i].own;
@@ -371,8 +390,8 @@ __global__ void __launch_bounds__(kThreads) read4_kernel(Read4Args a) {
     v = eight_values<ET>(((const uint32_t*)a.v_codes)[at], scale_of(a.v_scales[at / 4]));
   }
   const int64_t to = (int64_t)t * a.per_token.d + in;
-  ((u32x4*)a.k_out)[to] = k;
-  ((u32x4*)a.v_out)[to] = v;
+  __builtin_nontemporal_store(k, (u32x4*)a.k_out + to);
+  __builtin_nontemporal_store(v, (u32x4*)a.v_out + to);
 }
 
 template <typename ET, bool FOUR, Pairs PAIRS>
