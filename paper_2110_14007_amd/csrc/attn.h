@@ -98,6 +98,9 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int32_t s) {
                          PAGED && real ? a.cached[s] : 0);
 }
 
+// A value that all lanes hold, as a scalar.
+__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // 16 zero bytes: what a lane stages for a key, or a piece of one, that does not exist.
 static __device__ const uint4 kZeros = {0, 0, 0, 0};
 
@@ -167,11 +170,13 @@ struct Stager {
   int32_t seq, start, seen;  // keys from `seen` on are not loaded
   int32_t first = INT32_MIN / 2, entry = 0;
 
-  __device__ Stager(const AttnArgs& args, uint32_t hd) : a(args), head(hd) {}
+  const int lane;
+
+  __device__ Stager(const AttnArgs& args, uint32_t hd, int ln = threadIdx.x & 63)
+      : a(args), head(hd), lane(ln) {}
 
   // Row of the cache (or of k) of key j0 + lane; ~0: none.
   __device__ __forceinline__ uint32_t place(int32_t j0, int32_t keys) {
-    const int lane = threadIdx.x & 63;
     const int32_t j = j0 + lane;
     if constexpr (PAGED) {
       const int32_t lo = (int32_t)div_by((uint32_t)j0, a.page);
@@ -197,7 +202,7 @@ struct Stager {
     const int32_t pg = (int32_t)div_by((uint32_t)j, a.page);
     if (pg < first || pg - first >= 64) {
       first = max(pg - 16, 0);
-      const int32_t e = first + (int32_t)(threadIdx.x & 63);
+      const int32_t e = first + lane;
       entry = e < a.cols ? a.table[(int64_t)seq * a.cols + e] : -1;
       asm volatile("" : "+v"(entry));  // waited for here, not by every stage's first use
     }
@@ -209,7 +214,6 @@ struct Stager {
 
   // Rows r0 .. r0 + kRowsLoad - 1 of a K (or V) stage that begins at LDS address `to`.
   __device__ __forceinline__ void load_one(bool isk, uint32_t at, int r0, uint32_t to) const {
-    const int lane = threadIdx.x & 63;
     const int r = r0 + lane / kPieces, pc = lane % kPieces;
     const uint32_t row = (uint32_t)__shfl((int)at, r, 64);
     const int c = 8 * (pc ^ (isk ? swizzle_k<DP>(r) : swizzle_v<DP>(r)));
@@ -225,7 +229,6 @@ struct Stager {
   // Rows r0 .. r0 + kRowsLoad - 1 of a stage over pages whose K begins at LDS address k and V at v,
   // read by no other wave; at: place().
   __device__ __forceinline__ void load(uint32_t at, int r0, uint32_t k, uint32_t v) const {
-    const int lane = threadIdx.x & 63;
     const int r = r0 + lane / kPieces, pc = lane % kPieces;
     const uint32_t row = (uint32_t)__shfl((int)at, r, 64);
     const int ck = 8 * (pc ^ swizzle_k<DP>(r)), cv = 8 * (pc ^ swizzle_v<DP>(r));
@@ -295,13 +298,13 @@ __device__ __forceinline__ typename Frag<ET>::V values(const uint16_t* vs, int r
 
 // Whether a V stage of 32 keys holds an infinity or a NaN, the same for the whole wave.
 template <typename ET, int DP>
-__device__ __forceinline__ bool holds_nonfinite(const uint16_t* vs) {
+__device__ __forceinline__ bool holds_nonfinite(const uint16_t* vs, int lane = threadIdx.x & 63) {
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
   u16x2 top = {0, 0};
 #pragma unroll
   for (int i = 0; i < 32 * DP / 512; ++i) {
-    const u32x4 v = *(const u32x4*)(vs + 8 * (64 * i + (threadIdx.x & 63)));
+    const u32x4 v = *(const u32x4*)(vs + 8 * (64 * i + lane));
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu));
@@ -311,9 +314,10 @@ __device__ __forceinline__ bool holds_nonfinite(const uint16_t* vs) {
 
 // Clears those of the stage's values, the thread's share of it (from first, every step threads).
 template <typename ET, int DP>
-__device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int step) {
+__device__ __forceinline__ void clear_nonfinite(uint16_t* vs, int first, int step,
+                                                int lane = threadIdx.x & 63) {
   constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
-  for (int i = first + (threadIdx.x & 63); i < 32 * DP; i += step)
+  for (int i = first + lane; i < 32 * DP; i += step)
     if ((vs[i] & 0x7fff) >= kInf) vs[i] = 0;
 }
 
@@ -362,7 +366,7 @@ template <typename ET, int DP, bool PAGED, bool FOUR = false, typename OT, typen
 __device__ __forceinline__ void restore_nonfinite(ST& st, OT* out, int32_t step, const Seq& s,
                                                   int32_t m0, int32_t j0, int32_t j1, float sum) {
   const AttnArgs& a = st.a;
-  const int lane = threadIdx.x & 63;
+  const int lane = st.lane;
   constexpr uint16_t kInf = std::is_same<ET, _Float16>::value ? 0x7c00 : 0x7f80;
   const uint64_t sound = __ballot(finite(sum));
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the stores that this one follows
@@ -439,9 +443,10 @@ __device__ __forceinline__ float log_sum(float m, float sum) {
 // the accumulators a lane could write 8 bytes at a time only.
 template <typename ET, int DP, int W>
 __device__ __forceinline__ void store_rows(const f32x16 (&o)[W / 32], float f, ET* out, int64_t at,
-                                           int32_t dim, uint16_t* lds) {
+                                           int32_t dim, uint16_t* lds,
+                                           int lane = threadIdx.x & 63) {
   constexpr int kPieces = DP / 8, kRowsStore = 64 / kPieces;  // 16-byte pieces; rows of a store
-  const int lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
+  const int col = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int d = 0; d < W / 32; ++d)
 #pragma unroll

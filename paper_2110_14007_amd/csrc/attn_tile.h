@@ -119,19 +119,9 @@ __device__ __forceinline__ AttnArgs own_args() {
   return __builtin_bit_cast(AttnArgs, v);
 }
 
-// A wave's share of a 4-bit stage of keys or values, on its way from memory to LDS: eight rows of
-// eight lanes, DP / 8 elements a lane, all of one block.
-template <int DP>
-struct Codes {
-  typedef uint32_t W __attribute__((ext_vector_type(DP / 64)));
-  W words;
-  uint32_t scale;
-};
-
 // W: the elements of a row that the products take, of the DP that its stages have room for.  FULL:
-// the rows have DP elements.  FOUR: the pages are a 4-bit cache's: a wave loads its rows' codes into
-// registers a turn ahead, and writes them as 16-bit elements into the stages.
-template <typename ET, int DP, int W, bool FULL, bool PAGED, bool FOUR>
+// the rows have DP elements.
+template <typename ET, int DP, int W, bool FULL, bool PAGED>
 __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     tile_kernel(AttnArgs a) {
   using V8 = typename Frag<ET>::V;
@@ -146,7 +136,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // The last workgroups, if any, are the token workers': they read the memory while the tiles
   // that are left compute.
-  if constexpr (PAGED && !FOUR) {
+  if constexpr (PAGED) {
     if (blockIdx.x >= a.tile_groups) {
       if (wave < tile_workers<DP>())
         token_work<ET, DP>(own_args(), (blockIdx.x - a.tile_groups) * tile_workers<DP>() + wave,
@@ -245,39 +235,6 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   };
   constexpr std::true_type kIsK{};
   constexpr std::false_type kIsV{};
-  // The same over a 4-bit cache in two steps: stage i's codes into registers, and those as elements
-  // into buffer `ring`.
-  Codes<DP> kcodes, vcodes;
-  const int row4 = wave * kRowsWave + lane / 8, e4 = DP / 8 * (lane % 8);
-  auto fetch = [&](auto ISK, int32_t i) __attribute__((always_inline)) {
-    constexpr bool isk = decltype(ISK)::value;
-    if (i >= count) return;
-    uint32_t row;
-    if (i < fast) {
-      row = st.row_of(first + i * kKeys);
-      row = row == ~0u ? row : row + lane / 8;
-    } else {
-      row = (uint32_t)__shfl((int)st.place((jb + i) * kKeys, kKeys), row4, 64);
-    }
-    const bool ok = row != ~0u && (FULL || e4 < a.dim);
-    const int32_t dim = FULL ? DP : a.dim;
-    const uint8_t* const c = (const uint8_t*)(isk ? a.k : a.v) + (int64_t)row * (dim / 2) + e4 / 2;
-    const uint8_t* const b = (isk ? a.k_scales : a.v_scales) + (int64_t)row * (dim / 32) + e4 / 32;
-    Codes<DP>& to = isk ? kcodes : vcodes;
-    to.words = load_global<typename Codes<DP>::W>(ok ? c : (const uint8_t*)&kZeros);
-    to.scale = load_global<uint8_t>(ok ? b : (const uint8_t*)&kZeros);
-  };
-  auto put = [&](auto ISK, int32_t i, int ring) __attribute__((always_inline)) {
-    constexpr bool isk = decltype(ISK)::value;
-    if (i >= count || (!FULL && e4 >= a.dim)) return;
-    const Codes<DP>& from = isk ? kcodes : vcodes;
-    uint16_t* const to = lds + kStage * (ring + (isk ? 0 : kRing)) + row4 * DP;
-    const int swizzle = isk ? swizzle_k<DP>(row4) : swizzle_v<DP>(row4);
-    const float scale = scale_of(from.scale);
-#pragma unroll
-    for (int x = 0; x < DP / 64; ++x)
-      *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>((uint32_t)from.words[x], scale);
-  };
 
   f32x16 o[DB];
 #pragma unroll
@@ -417,46 +374,24 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   f32x16 sa, sb;
   u32x4 pa[2], pb[2];
   pb[0] = pb[1] = u32x4{0, 0, 0, 0};
-  if constexpr (FOUR) {
-    fetch(kIsK, 0);
-    fetch(kIsV, 0);
-    put(kIsK, 0, 0);
-    put(kIsV, 0, 0);
-    fetch(kIsK, 1);
-    put(kIsK, 1, 1);
-    fetch(kIsK, 2);
-    put(kIsK, 2, 2);
-    fetch(kIsK, 3);
-    fetch(kIsV, 1);
-    mt::stage_barrier();
-  } else {
-    stage(kIsK, 0, 0);
-    stage(kIsK, 1, 1);
-    stage(kIsV, 0, 0);
-    stage(kIsK, 2, 2);
-    mt::dl_barrier<0>();
-  }
+  stage(kIsK, 0, 0);
+  stage(kIsK, 1, 1);
+  stage(kIsV, 0, 0);
+  stage(kIsK, 2, 2);
+  mt::dl_barrier<0>();
 #pragma unroll
   for (int r = 0; r < 16; ++r) sa[r] = 0.0f;
 #pragma unroll
   for (int c = 0; c < KC; ++c) sa = mfma<ET>(kfrag(0, c), q[c], sa);
   auto turn = [&](int32_t j, int r, f32x16& s, f32x16& n, const u32x4 (&p)[2],
                   u32x4 (&pn)[2]) __attribute__((always_inline)) {  // r: j % kRing
-    if constexpr (FOUR) {
-      mt::stage_barrier();
-      put(kIsK, j + 3, (r + 3) % kRing);
-      put(kIsV, j + 1, (r + 1) % kRing);
-      fetch(kIsK, j + 4);
-      fetch(kIsV, j + 2);
-    } else {
-      // The loads of the turn before stay in flight while there are as many as a turn issues.
-      if (j + 2 < count)
-        mt::dl_barrier<2 * kLoads>();
-      else
-        mt::dl_barrier<0>();
-      stage(kIsK, j + 3, (r + 3) % kRing);
-      stage(kIsV, j + 1, (r + 1) % kRing);
-    }
+    // The loads of the turn before stay in flight while there are as many as a turn issues.
+    if (j + 2 < count)
+      mt::dl_barrier<2 * kLoads>();
+    else
+      mt::dl_barrier<0>();
+    stage(kIsK, j + 3, (r + 3) % kRing);
+    stage(kIsV, j + 1, (r + 1) % kRing);
     if (j > open) clear(j - 1);
     step((jb + j) * kKeys, (r + 1) % kRing * kS, (r + kRing - 1) % kRing * kS, s, n, p, pn);
   };
@@ -491,7 +426,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
     if (mine) store_part<W>(o, a.tile_o + row * DP, h);
     if (mine && h == 0) a.tile_stat[row] = {mref, sum};
     if (restore)
-      restore_nonfinite<ET, DP, PAGED, FOUR>(st, a.tile_o + (row - col) * DP, DP, t, t.row0 + 32 * wave,
+      restore_nonfinite<ET, DP, PAGED>(st, a.tile_o + (row - col) * DP, DP, t, t.row0 + 32 * wave,
                                        jb * kKeys, (jb + count) * kKeys, sum);
     return;
   }
@@ -501,7 +436,7 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
   store_rows<ET, DP, W>(o, inverse(sum), (ET*)a.out, mine ? orow * a.dim : -1, a.dim,
                      lds + wave * 32 * DP);
   if (restore)
-    restore_nonfinite<ET, DP, PAGED, FOUR>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, jb * kKeys,
+    restore_nonfinite<ET, DP, PAGED>(st, (ET*)a.out, 0, t, t.row0 + 32 * wave, jb * kKeys,
                                      (jb + count) * kKeys, sum);
 }
 
@@ -527,17 +462,17 @@ __global__ void __launch_bounds__(256) tile_join_kernel(AttnArgs a) {
   }
 }
 
-template <typename ET, int DP, int W, bool FULL, bool PAGED, bool FOUR>
+template <typename ET, int DP, int W, bool FULL, bool PAGED>
 hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
   const int64_t slots = a.tile_slots;
   constexpr unsigned bytes = 2 * kRing * kKeys * DP * 2;  // K and V, 16 bits
-  const auto kern = tile_kernel<ET, DP, W, FULL, PAGED, FOUR>;
+  const auto kern = tile_kernel<ET, DP, W, FULL, PAGED>;
   if constexpr (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
-  const int64_t tokens = PAGED && !FOUR && a.skip_rows ? token_workers(DP) / tile_workers<DP>() : 0;
+  const int64_t tokens = PAGED && a.skip_rows ? token_workers(DP) / tile_workers<DP>() : 0;
   hipLaunchKernelGGL(kern, dim3((unsigned)(a.tile_groups + tokens)), dim3(64 * kWaves), bytes, s, a);
   if (a.tile_parts > 1)
     hipLaunchKernelGGL((tile_join_kernel<ET, DP, PAGED>),
@@ -545,16 +480,15 @@ hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename ET, bool PAGED, bool FOUR>
+template <typename ET, bool PAGED>
 hipError_t launch_tile(const AttnArgs& a, hipStream_t s) {
-  if (a.dim < 64) return launch_tile<ET, 64, 64, false, PAGED, FOUR>(a, s);
-  if (a.dim == 64) return launch_tile<ET, 64, 64, true, PAGED, FOUR>(a, s);
-  if (a.dim <= 96) return launch_tile<ET, 128, 96, false, PAGED, FOUR>(a, s);
-  if constexpr (!FOUR)
-    if (a.dim < 128) return launch_tile<ET, 128, 128, false, PAGED, FOUR>(a, s);
-  if (a.dim == 128) return launch_tile<ET, 128, 128, true, PAGED, FOUR>(a, s);
-  if (a.dim < 256) return launch_tile<ET, 256, 256, false, PAGED, FOUR>(a, s);
-  return launch_tile<ET, 256, 256, true, PAGED, FOUR>(a, s);
+  if (a.dim < 64) return launch_tile<ET, 64, 64, false, PAGED>(a, s);
+  if (a.dim == 64) return launch_tile<ET, 64, 64, true, PAGED>(a, s);
+  if (a.dim <= 96) return launch_tile<ET, 128, 96, false, PAGED>(a, s);
+  if (a.dim < 128) return launch_tile<ET, 128, 128, false, PAGED>(a, s);
+  if (a.dim == 128) return launch_tile<ET, 128, 128, true, PAGED>(a, s);
+  if (a.dim < 256) return launch_tile<ET, 256, 256, false, PAGED>(a, s);
+  return launch_tile<ET, 256, 256, true, PAGED>(a, s);
 }
 
 }  // namespace attn

@@ -4,8 +4,7 @@
 namespace tod {
 
 hipError_t launch_attn_tile_f16(const AttnArgs& a, bool paged, hipStream_t s) {
-  return paged ? attn::launch_tile<_Float16, true, false>(a, s)
-               : attn::launch_tile<_Float16, false, false>(a, s);
+  return paged ? attn::launch_tile<_Float16, true>(a, s) : attn::launch_tile<_Float16, false>(a, s);
 }
 
 }  // namespace tod

@@ -41,9 +41,6 @@ __device__ __forceinline__ f32x4 mfma16(typename Frag<ET>::V a, typename Frag<ET
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// A value that all lanes hold, as a scalar.
-__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
-
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 template <typename F>
 __device__ __forceinline__ float over_quarters(float v, F&& f) {

@@ -74,6 +74,13 @@ struct Read4Args {
   int32_t kv_heads;
 };
 
+// Where a worker's share of the tiles over a 4-bit cache begins: the tile, by its place in the line
+// of all tiles (-1: the worker has no share), and the stage of it.
+struct TileCut {
+  int64_t x;
+  int32_t seq, tile, head, stage, stages, unused;
+};
+
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;  // strides in elements
@@ -99,7 +106,9 @@ struct AttnArgs {
   int32_t part_keys;    // fewest keys of a split
   float2* tile_stat;    // [tiles of all heads, parts, rows]
   float* tile_o;        // [tiles of all heads, parts, rows, padded dim]
-  const uint8_t *k_scales, *v_scales;  // of a 4-bit cache, whose codes are k and v
+  // A 4-bit cache: its codes are k and v.
+  const uint8_t *k_scales, *v_scales;
+  TileCut* tile_cut;  // [workers]; each has two tiles' rows in tile_stat and tile_o
 };
 
 // Packed rows that the token kernel takes: a product's 32 columns.  (96 tokens over caches of 100
@@ -110,6 +119,8 @@ constexpr int kTokenMaxRows = 32;
 // TB/s with four a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
 constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
+// Workers of the tiles over a 4-bit cache: as many workgroups as fit on 256 compute units at once.
+constexpr int32_t tile4_workers(int32_t dim) { return dim > 128 ? 256 : dim > 64 ? 512 : 768; }
 // Over a 4-bit cache: three waves on each of 1,024 SIMDs, two for more than 128 elements.
 constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 2048 : 3072; }
 

@@ -111,7 +111,7 @@ struct Plan {
   int64_t tile_slots;
   bool tile;  // some sequence may have more rows than the token kernel takes
   bool fits;  // every launch has fewer than 2^32 threads
-  size_t line, token_stat, token_o, tile_stat, tile_o, total;
+  size_t line, token_stat, token_o, tile_stat, tile_o, tile_cut, total;
 };
 
 enum class Form { kPrompt, kPaged, kPaged4 };  // whole prompts; pages; pages of a 4-bit cache
@@ -144,7 +144,13 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
   }
   p.tile_parts = 1;
   p.tile_slots = tokens * group / 128 + n_seq + 1;
-  if (p.tile) {
+  if (p.tile && form == Form::kPaged4) {
+    // Two pieces of a tile for every worker.
+    const int64_t workers = tod::tile4_workers(o.dim);
+    p.tile_stat = take(workers * 2 * 128 * 8);
+    p.tile_o = take(workers * 2 * 128 * dp * 4);
+    p.tile_cut = take(workers * (int64_t)sizeof(tod::TileCut));
+  } else if (p.tile) {
     // Two workgroups on every compute unit, from the rows that there are; slots beside them, one a
     // sequence and head, stay empty but count towards the 2,048 workgroups.  A prompt has no more
     // keys than tokens; a split has at least 512.  (512 tokens after 60,007, 2 heads of 128: 8 parts
@@ -186,7 +192,9 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, Form for
   a->token_o = (float*)(base + p.token_o);
   a->tile_slots = (int32_t)p.tile_slots;
   a->tile_parts = p.tile_parts;
-  a->tile_groups = (uint32_t)(p.tile_slots * o.kv_heads * p.tile_parts);
+  a->tile_groups = form == Form::kPaged4 ? (uint32_t)tod::tile4_workers(o.dim)
+                                         : (uint32_t)(p.tile_slots * o.kv_heads * p.tile_parts);
+  a->tile_cut = (tod::TileCut*)(base + p.tile_cut);
   a->parts_div = tod::fast_div((uint32_t)p.tile_parts);
   a->part_keys = kPartKeys;
   a->tile_stat = (float2*)(base + p.tile_stat);
