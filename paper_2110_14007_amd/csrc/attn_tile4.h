@@ -175,14 +175,21 @@ struct Codes {
 
 constexpr int kRing4 = 2;  // stages of K, and of V, in LDS
 
+// Pieces of V rows: as swizzle_v for the transposing read; that neighbouring rows differ in the lowest
+// bit too puts a wave's writes, every other piece of two rows at a time, on different banks.
+template <int DP>
+__device__ __forceinline__ int swizzle_v4(int row) {
+  return DP == 64 ? 0 : (row & 3) << 1 | (row & 1);
+}
+
 // A workgroup's work on `count` stages, at least one, of a tile from jb on: the tile's output, or partial results into
 // the rows from part_row on where that is not below 0.  W: the elements of a row that the products
 // take, of the DP that its stages have room for.  FULL: the rows have DP elements.  EVEN: pages hold
 // whole groups of eight rows.
 template <typename ET, int DP, int W, bool FULL, bool EVEN>
-__device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, const uint32_t head,
-                                           const int32_t jb, const int32_t count,
-                                           const int64_t part_row, uint16_t* const lds) {
+__device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given, uint32_t head,
+                                           int32_t jb, int32_t count, const int64_t part_row,
+                                           uint16_t* const lds) {
   using V8 = typename Frag<ET>::V;
   constexpr int kStage = kKeys * DP;         // elements of a stage
   constexpr int kRowsWave = kKeys / kWaves;  // rows of a stage that a wave loads
@@ -191,6 +198,20 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
   asm volatile("" : "+v"(tid));  // what follows from it is formed for each tile, and not kept
   const int lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = uniform(tid >> 6);
+
+  // (All of the workgroup's: kept in scalar registers.)
+  Tile t = given;
+  t.start = uniform(t.start);
+  t.n = uniform(t.n);
+  t.keys = uniform(t.keys);
+  t.shift = uniform(t.shift);
+  t.seq = uniform(t.seq);
+  t.row0 = uniform(t.row0);
+  t.rows = uniform(t.rows);
+  t.seen = uniform(t.seen);
+  head = (uint32_t)uniform((int32_t)head);
+  jb = uniform(jb);
+  count = uniform(count);
 
   // This lane's query row, and the last key that it sees.
   const int32_t m = min(t.row0 + 32 * wave + col, t.rows - 1);
@@ -242,14 +263,15 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
       to.scale = load_global<uint8_t>(ok ? b + (uint64_t)row * row_scales + in4 / 32 : zeros);
     }
   };
-  // Stage i's, found in `row`.  A value that does not exist may not meet a weight, not even one of 0.
-  auto put = [&](auto ISK, int32_t i, uint32_t row, int ring, const Codes<DP>& from)
+  // Word x of stage i's codes, found in `row`.  A value that does not exist may not meet a weight, not
+  // even one of 0.
+  auto put = [&](auto ISK, int x, int32_t i, uint32_t row, int ring, const Codes<DP>& from)
       __attribute__((always_inline)) {
     constexpr bool isk = decltype(ISK)::value;
     if (!FULL && e4 >= a.dim) return;
     uint16_t* const to = lds + kStage * (ring + (isk ? 0 : kRing4)) + row4 * DP;
-    const int swizzle = isk ? swizzle_k<DP>(row4) : swizzle_v<DP>(row4);
-    typename Codes<DP>::W w = from.words;
+    const int swizzle = isk ? swizzle_k<DP>(row4) : swizzle_v4<DP>(row4);
+    uint32_t w = from.words[x];
     float scale;
     if constexpr (EVEN) {
       w &= row == ~0u ? 0u : ~0u;
@@ -259,9 +281,7 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
     } else {
       scale = scale_of(from.scale);
     }
-#pragma unroll
-    for (int x = 0; x < DP / 64; ++x)
-      *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>((uint32_t)w[x], scale);
+    *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>(w, scale);
   };
   constexpr std::true_type kIsK{};
   constexpr std::false_type kIsV{};
@@ -292,7 +312,7 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
   for (int d = 0; d < 2; ++d) {
     const int row = 4 * h + (lane & 15) / 4;
     const int piece = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    va[d] = lbase + 2 * (kRing4 * kStage + row * DP + 8 * (piece ^ swizzle_v<DP>(row)) + 4 * (lane & 1));
+    va[d] = lbase + 2 * (kRing4 * kStage + row * DP + 8 * (piece ^ swizzle_v4<DP>(row)) + 4 * (lane & 1));
   }
   // at: byte offset of the 32 (K) or 16 (V) rows in the ring.
   auto kfrag = [&](int at, int c) {
@@ -309,10 +329,10 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
   // One step: softmax of the 32 keys from j0 on (scores s -> weights pn), the scores of the next
   // 32 (n; at kat in the K ring) and the product of the 32 before (weights p; at vat in the V
   // ring).  The three do not depend on each other.  They are laid out in slots of one MFMA, the
-  // LDS reads of the MFMA kAhead slots on, and a share of the exponentials.
+  // LDS reads of the MFMA kAhead slots on, a share of the exponentials, and of the staging.
   constexpr int kSlots = KC + 2 * DB, kAhead = DP > 128 ? 2 : 4, kCheck = 2;
-  auto step = [&](int32_t j0, int kat, int vat, f32x16& s, f32x16& n,
-                  const u32x4 (&p0)[2], u32x4 (&pn)[2]) __attribute__((always_inline)) {
+  auto step = [&](int32_t j0, int kat, int vat, f32x16& s, f32x16& n, const u32x4 (&p0)[2],
+                  u32x4 (&pn)[2], auto&& staging) __attribute__((always_inline)) {
     u32x4 p[2] = {p0[0], p0[1]};
     V8 fr[kSlots];
     auto read = [&](auto I) __attribute__((always_inline)) {
@@ -382,6 +402,7 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
           few += x1;
           pn[e / 4][e % 4] = pack2<ET>(x0, x1);
         }
+        staging(I);
         __builtin_amdgcn_sched_barrier(0);
       }
     });
@@ -413,8 +434,11 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
     fetch(kIsK, r1, k1);
     fetch(kIsK, r2, kcodes);
     fetch(kIsV, r0, vcodes);
-    put(kIsK, 0, r0, 0, k0);
-    put(kIsK, 1, r1, 1, k1);
+#pragma unroll
+    for (int x = 0; x < DP / 64; ++x) {
+      put(kIsK, x, 0, r0, 0, k0);
+      put(kIsK, x, 1, r1, 1, k1);
+    }
     mt::stage_barrier();
   }
 #pragma unroll
@@ -424,17 +448,31 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& t, con
   auto turn = [&](int32_t j, int r, f32x16& s, f32x16& n, const u32x4 (&p)[2],
                   u32x4 (&pn)[2]) __attribute__((always_inline)) {  // r: j % 2
     mt::stage_barrier();
-    put(kIsK, j + 2, r2, r, kcodes);
-    put(kIsV, j, r0, r, vcodes);
+    if (j > open) clear(j - 1);
+    // K j + 2 and V j go to LDS word by word, then the loads of those after them begin.
+    constexpr int kWords = DP / 64, kFirst = kCheck + 1, kLast = kSlots - 2;
+    uint32_t next = 0;
+    step((jb + j) * kKeys, (1 - r) * kS, (1 - r) * kS, s, n, p, pn,
+         [&](auto I) __attribute__((always_inline)) {
+           constexpr int i = decltype(I)::value;
+           mt::static_for<0, 2 * kWords>([&](auto X) __attribute__((always_inline)) {
+             constexpr int x = decltype(X)::value;
+             if constexpr (i == kFirst + (DP > 128 ? 0 : x * (kLast - kFirst) / (2 * kWords))) {
+               if constexpr (x < kWords)
+                 put(kIsK, x, j + 2, r2, r, kcodes);
+               else
+                 put(kIsV, x - kWords, j, r0, r, vcodes);
+             }
+           });
+           if constexpr (i == kLast) next = find(j + 3);
+           if constexpr (i == kSlots - 1) {
+             fetch(kIsK, next, kcodes);
+             fetch(kIsV, r1, vcodes);
+           }
+         });
     r0 = r1;
     r1 = r2;
-    r2 = find(j + 3);
-    __builtin_amdgcn_sched_barrier(0);  // into the registers that the conversions left
-    fetch(kIsK, r2, kcodes);
-    fetch(kIsV, r0, vcodes);
-    __builtin_amdgcn_sched_barrier(0);
-    if (j > open) clear(j - 1);
-    step((jb + j) * kKeys, (1 - r) * kS, (1 - r) * kS, s, n, p, pn);
+    r2 = next;
   };
   // Scores and weights change places every turn: a pass of the loop takes an even number.
   for (int32_t j = 0; j < count; j += 2) {
