@@ -16,11 +16,12 @@
 #pragma once
 
 #include "attn_tile.h"
+#include "attn_token4.h"
 
 namespace tod {
 namespace attn {
 
-constexpr int32_t kTileWeight = 128;  // of a tile's start and stores, in keys
+constexpr int32_t kTileWeight = 256;  // of a tile's start and stores, in keys
 constexpr int32_t kShareKeys = 512;   // least weight of a worker's share, where there are few tiles
 constexpr int32_t kLeastPiece = 4;    // stages that a cut leaves on either side
 constexpr int32_t kWhole = 8;         // tiles of which a share holds more are not cut
@@ -517,6 +518,13 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
                                           (jb + count) * kKeys, sum);
 }
 
+// Where a worker is in its share: the tile and its first stage, and the share's end.
+struct TilePlace {
+  Seq q;
+  int32_t seq, tile, head, stage, end_seq, end_tile, end_head, end_stage;
+  int32_t first;  // 1: the share's first tile
+};
+
 // A piece without stages, where others of its tile follow: rows of weight 0.
 template <int DP>
 __device__ __forceinline__ void clear_piece(const AttnArgs& a, int64_t row) {
@@ -538,50 +546,77 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a, const Tile& t, int
   }
 }
 
+// A worker's share of the tiles.
 template <typename ET, int DP, int W, bool FULL, bool EVEN>
-__global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
-    tile4_kernel(AttnArgs a) {
-  extern __shared__ __align__(16) uint16_t lds[];  // stages of K, then as many of V
+__device__ __forceinline__ void tile4_share(const AttnArgs& a, uint16_t* const lds) {
   // Neighbours in the line, which read the same keys, run on the same XCD (its workgroups are those
   // of every eighth number).
   const int32_t each = (int32_t)a.tile_groups / 8;
   const int32_t w = (int32_t)(blockIdx.x % 8) * each + (int32_t)(blockIdx.x / 8);
   const TileLine line(a);
-  const TileCut from = line.cut(a, w), to = line.cut(a, w + 1);
+  const TileCut from = line.cut(a, w), end = line.cut(a, w + 1);
   if (threadIdx.x == 0) a.tile_cut[w] = from;
   if (from.x < 0) return;
-  int32_t s = from.seq, i = from.tile, head = from.head, j0 = from.stage;
-  Seq q = line.seq(a, s);
-  bool first = true;
+  // Where the worker is in its share lies in LDS meanwhile: a tile's work needs all registers.
+  typedef __attribute__((address_space(3))) TilePlace* place;
+  const place at = (place)(__attribute__((address_space(3))) uint16_t*)(lds + 2 * kRing4 * kKeys * DP);
+  TilePlace now = {line.seq(a, from.seq), from.seq, from.tile, from.head, from.stage,
+                   end.seq, end.tile, end.head, end.stage, 1};
   for (;;) {
-    const Tile t = tile_at(a, s, q, i);
-    const bool last = s == to.seq && head == to.head && i == to.tile;
-    const int32_t j1 = last ? to.stage : t.stages;
+    const Tile t = tile_at(a, now.seq, now.q, now.tile);
+    const bool last = now.seq == now.end_seq && now.head == now.end_head && now.tile == now.end_tile;
+    const int32_t j0 = now.stage, j1 = last ? now.end_stage : t.stages;
     const bool whole = j0 == 0 && j1 == t.stages;
-    const int64_t row = (2 * (int64_t)w + !first) * kRows;
+    const int64_t row = (2 * (int64_t)w + !now.first) * kRows;
     if (t.stages == 0) {
-      if (!last) clear_rows<ET>(a, t, head);
+      if (!last) clear_rows<ET>(a, t, now.head);
     } else if (j0 < j1) {
-      tile4_work<ET, DP, W, FULL, EVEN>(own_args(), t, (uint32_t)head, j0, j1 - j0, whole ? -1 : row,
-                                        lds);
+      if (threadIdx.x == 0) *(TilePlace*)at = now;
+      tile4_work<ET, DP, W, FULL, EVEN>(own_args(), t, (uint32_t)now.head, j0, j1 - j0,
+                                        whole ? -1 : row, lds);
       mt::stage_barrier();  // the stages are free for the next tile's
+      now = *(const TilePlace*)at;
+      mt::stage_barrier();  // read before it is written again
     } else if (last && j0 > 0 && j0 < t.stages) {
       clear_piece<DP>(a, row);
     }
     if (last) return;
     // The next tile: of this head, of the next, of the next sequence that has any.
-    first = false;
-    j0 = 0;
-    if (++i * kRows >= t.rows) {
-      i = 0;
-      if (++head == a.kv_heads) {
-        head = 0;
+    now.first = 0;
+    now.stage = 0;
+    if (++now.tile * kRows >= now.q.n * (int32_t)a.group.d) {
+      now.tile = 0;
+      if (++now.head == a.kv_heads) {
+        now.head = 0;
         do {
-          if (++s > a.n_seq) return;
-          q = seq_of<true>(a, s);
-          q = {uniform(q.start), uniform(q.n), uniform(q.keys), uniform(q.shift)};
-        } while (tiles_of(a, s, q).count == 0);
+          if (++now.seq > a.n_seq) return;
+          now.q = seq_of<true>(a, now.seq);
+        } while (uniform(tiles_of(a, now.seq, now.q).count) == 0);
       }
+    }
+  }
+}
+
+// The waves are the token workers too, where a call has both.  Of the workgroups that share a compute
+// unit some begin with the tokens and some with the tiles, so that the memory is read while products
+// are formed.
+template <typename ET, int DP, int W, bool FULL, bool EVEN>
+__global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
+    tile4_kernel(AttnArgs a) {
+  extern __shared__ __align__(16) uint16_t lds[];  // stages of K, as many of V, the place
+  const bool late = blockIdx.x >= a.tile_groups / 2;
+  for (int turn = 0; turn < 2; ++turn) {
+    if (turn) mt::stage_barrier();  // the LDS is free
+    if (late == (turn == 0)) {
+      if (a.ride) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));  // what follows from it is formed here, and not kept
+        const int wave = uniform(tid >> 6);
+        token4_work<ET, DP, 1, EVEN>(own_args(), blockIdx.x * kWaves + wave, a.tile_groups * kWaves,
+                                     lds + wave * (32 * DP), tid & 63);
+      }
+    } else {
+      tile4_share<ET, DP, W, FULL, EVEN>(own_args(), lds);
     }
   }
 }
@@ -656,9 +691,9 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
 
 // Joins the pieces of the cut tiles.  A tile of n pieces is cut by n - 1 workers' beginnings; each of
 // them stands for as many workgroups, which share the tile's rows with the other beginnings'.
-constexpr int kJoinGroups = 4, kJoinThreads = 512, kJoinEach = 4;
+constexpr int kJoinGroups = 4, kJoinThreads = 64 * kJoinWaves, kJoinEach = 4;
 template <typename ET, int DP>
-__global__ void __launch_bounds__(kJoinThreads) tile4_join_kernel(AttnArgs a) {
+__device__ __forceinline__ void tile4_join(const AttnArgs& a) {
   const int32_t w = (int32_t)(blockIdx.x / kJoinGroups) + 1, last = (int32_t)a.tile_groups - 1;
   const int lane = threadIdx.x & 63;
   const TileCut c = a.tile_cut[w];
@@ -705,19 +740,42 @@ __global__ void __launch_bounds__(kJoinThreads) tile4_join_kernel(AttnArgs a) {
     join(std::integral_constant<int, kJoinEach>{});
 }
 
+// The joins of the tiles and, behind them, of the tokens that the same kernel worked on.
+template <typename ET, int DP, bool ALL>
+__global__ void __launch_bounds__(kJoinThreads) tile4_join_kernel(AttnArgs a) {
+  const uint32_t tiles = (a.tile_groups - 1) * kJoinGroups;
+  if (blockIdx.x < tiles) {
+    tile4_join<ET, DP>(a);
+  } else if constexpr (ALL) {
+    __shared__ Joined<DP> left[kJoinWaves][64];
+    token_join<ET, DP, true>(a, blockIdx.x - tiles, a.tile_groups * kWaves, left);
+  } else {
+    token_join<ET, DP, false>(a, blockIdx.x - tiles, a.tile_groups * kWaves, nullptr);
+  }
+}
+
 template <typename ET, int DP, int W, bool FULL>
 hipError_t launch_tile4(const AttnArgs& a, hipStream_t s) {
-  constexpr unsigned bytes = 2 * kRing4 * kKeys * DP * 2;  // K and V, 16 bits
-  const auto kern = a.page.d % 8 == 0 ? tile4_kernel<ET, DP, W, FULL, true>
-                                      : tile4_kernel<ET, DP, W, FULL, false>;
+  constexpr unsigned bytes = 2 * kRing4 * kKeys * DP * 2 + 64;  // K and V, 16 bits; the place
+  // Blocks of 16 rows, for the tokens; the tiles need eight.
+  const auto kern = a.page.d % 16 == 0 ? tile4_kernel<ET, DP, W, FULL, true>
+                                       : tile4_kernel<ET, DP, W, FULL, false>;
   if constexpr (bytes > 65536) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kern, dim3(a.tile_groups), dim3(64 * kWaves), bytes, s, a);
-  hipLaunchKernelGGL((tile4_join_kernel<ET, DP>), dim3((a.tile_groups - 1) * kJoinGroups),
-                     dim3(kJoinThreads), 0, s, a);
+  const unsigned tiles = (a.tile_groups - 1) * kJoinGroups;
+  const int64_t pairs = a.ride ? (int64_t)a.n_seq * a.kv_heads : 0;
+  // (As launch_token_join has it.)
+  if (16 * pairs <= (int64_t)a.tile_groups * kWaves)
+    hipLaunchKernelGGL((tile4_join_kernel<ET, DP, true>),
+                       dim3(tiles + (unsigned)pairs * (unsigned)a.skip_rows), dim3(kJoinThreads), 0,
+                       s, a);
+  else
+    hipLaunchKernelGGL((tile4_join_kernel<ET, DP, false>), dim3(tiles + (unsigned)pairs),
+                       dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 

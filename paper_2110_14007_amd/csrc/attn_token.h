@@ -340,11 +340,13 @@ __global__ void __launch_bounds__(64) token_kernel(AttnArgs a) {
 // Joins the pieces of a (sequence, key / value head) pair.  ALL: a workgroup of kJoinWaves waves
 // takes one of its packed rows, and each wave an equal part of the row's pieces.  Otherwise it
 // takes all of the pair's rows, a wave a row at a time.
+// left: LDS for a row of every wave (ALL).
 constexpr int kJoinWaves = 8;
-template <typename ET, int DP, bool ALL, uint32_t grid>
-__global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a) {
-  const uint32_t row = ALL ? blockIdx.x % (uint32_t)a.skip_rows : 0;
-  const uint32_t pair = ALL ? blockIdx.x / (uint32_t)a.skip_rows : blockIdx.x;
+template <typename ET, int DP, bool ALL>
+__device__ __forceinline__ void token_join(const AttnArgs& a, const uint32_t block,
+                                           const uint32_t grid, Joined<DP> (*left)[64]) {
+  const uint32_t row = ALL ? block % (uint32_t)a.skip_rows : 0;
+  const uint32_t pair = ALL ? block / (uint32_t)a.skip_rows : block;
   const uint32_t s = div_by(pair, a.heads_div), head = pair - s * a.heads_div.d;
   const int64_t before = a.token_line[s], after = a.token_line[s + 1];
   const int64_t all = a.token_line[a.n_seq] * a.kv_heads, stages = after - before;
@@ -370,7 +372,6 @@ __global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a)
   };
   const int wave = (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if constexpr (ALL) {
-    __shared__ Joined<DP> left[kJoinWaves][64];
     Joined<DP> j = join((int32_t)row, pieces * wave / kJoinWaves, pieces * (wave + 1) / kJoinWaves);
     left[wave][lane] = j;
     __syncthreads();
@@ -389,6 +390,16 @@ __global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a)
     store((int32_t)row, j);
   } else {
     for (int32_t r = wave; r < rows; r += kJoinWaves) store(r, join(r, 0, pieces));
+  }
+}
+
+template <typename ET, int DP, bool ALL, uint32_t grid>
+__global__ void __launch_bounds__(64 * kJoinWaves) token_join_kernel(AttnArgs a) {
+  if constexpr (ALL) {
+    __shared__ Joined<DP> left[kJoinWaves][64];
+    token_join<ET, DP, true>(a, blockIdx.x, grid, left);
+  } else {
+    token_join<ET, DP, false>(a, blockIdx.x, grid, nullptr);
   }
 }
 

@@ -109,12 +109,12 @@ __device__ __forceinline__ int element4(int i, int g) {
 // EVEN: pages hold whole blocks of 16 keys, so that the wave finds a block by one address.
 template <typename ET, int DP, int NB, bool EVEN>
 __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t worker,
-                                            uint16_t* const lds) {
-  constexpr uint32_t grid = (uint32_t)token4_workers(DP);
+                                            const uint32_t grid, uint16_t* const lds,
+                                            const int lane = threadIdx.x & 63) {
   constexpr int KT = token4_tiles<DP>(), KEYS = token4_keys<DP>(), C = DP / 32, DB = DP / 16;
   using V8 = typename Frag<ET>::V;
   using L4 = Lane4<DP>;
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int n = lane & 15, g = lane >> 4;
 
   const Share mine = deal<KEYS>(a, worker, grid);
   int64_t at = mine.at, off = mine.off;
@@ -156,7 +156,7 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
     }
     const int32_t wlo = uniform(limit[0]);
 
-    Stager<ET, DP, true> st(a, head);
+    Stager<ET, DP, true> st(a, head, lane);
     st.seq = s;
     st.start = sq.start;
     st.seen = sq.keys;
@@ -340,9 +340,9 @@ __device__ __forceinline__ void token4_work(const AttnArgs& a, const uint32_t wo
         // A value that is not finite must not meet the zero weight of a row that does not see it.
         if (edge && rows > (int32_t)a.group.d) {
           asm volatile("" ::: "memory");  // (the stage is not read where it need not be)
-          if (holds_nonfinite<ET, DP>(lds)) {
+          if (holds_nonfinite<ET, DP>(lds, lane)) {
 #pragma unroll 1
-            for (int i = 0; i < 32 * DP; i += 512) clear_nonfinite<ET, 16>(lds + i, 0, 64);
+            for (int i = 0; i < 32 * DP; i += 512) clear_nonfinite<ET, 16>(lds + i, 0, 64, lane);
             cleared = true;
           }
         }
@@ -463,7 +463,7 @@ constexpr int token4_waves() { return DP == 256 ? NB == 1 ? 2 : 1 : NB == 1 ? 3 
 template <typename ET, int DP, int NB, bool EVEN>
 __global__ void __launch_bounds__(64, (token4_waves<DP, NB>())) token4_kernel(AttnArgs a) {
   __shared__ __align__(16) uint16_t lds[32 * DP];
-  token4_work<ET, DP, NB, EVEN>(a, blockIdx.x, lds);
+  token4_work<ET, DP, NB, EVEN>(a, blockIdx.x, (uint32_t)token4_workers(DP), lds);
 }
 
 template <typename ET, int DP>

@@ -109,6 +109,7 @@ struct AttnArgs {
   // A 4-bit cache: its codes are k and v.
   const uint8_t *k_scales, *v_scales;
   TileCut* tile_cut;  // [workers]; each has two tiles' rows in tile_stat and tile_o
+  int32_t ride, unused;  // 1: the tiles' waves are the token workers too
 };
 
 // Packed rows that the token kernel takes: a product's 32 columns.  (96 tokens over caches of 100

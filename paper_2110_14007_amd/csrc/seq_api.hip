@@ -136,8 +136,10 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
     const bool four = form == Form::kPaged4;
     const int64_t limit = four && p.tile && group <= 16 ? 16 : tod::kTokenMaxRows;
     p.skip_rows = (int32_t)(most < limit ? most : limit / group * group);
-    const int64_t rows =
-        2 * (four ? tod::token4_workers(o.dim) : tod::token_workers(o.dim)) * p.skip_rows;
+    const int64_t workers = !four   ? tod::token_workers(o.dim)
+                            : p.tile && p.skip_rows <= 16 ? 4 * (int64_t)tod::tile4_workers(o.dim)
+                                                          : tod::token4_workers(o.dim);
+    const int64_t rows = 2 * workers * p.skip_rows;
     p.line = take((n_seq + 1) * 8);
     p.token_stat = take(rows * 8);
     p.token_o = take(rows * dp * 4);
@@ -204,9 +206,10 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, Form for
   hipError_t e = hipSuccess;
   const bool paged = form == Form::kPaged;
   if (form == Form::kPaged4) {
+    a->ride = p.tile && p.skip_rows && p.skip_rows <= 16;
     if (p.tile)
       e = half ? tod::launch_attn_tile4_f16(*a, s) : tod::launch_attn_tile4_bf16(*a, s);
-    if (e == hipSuccess && p.skip_rows)
+    if (e == hipSuccess && p.skip_rows && !a->ride)
       e = half ? tod::launch_attn_token4_f16(*a, s) : tod::launch_attn_token4_bf16(*a, s);
     return launched(e, where);
   }
