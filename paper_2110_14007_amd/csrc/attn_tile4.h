@@ -24,6 +24,8 @@ namespace attn {
 constexpr int32_t kTileWeight = 256;  // of a tile's start and stores, in keys
 constexpr int32_t kShareKeys = 512;   // least weight of a worker's share, where there are few tiles
 constexpr int32_t kLeastPiece = 4;    // stages that a cut leaves on either side
+constexpr int32_t kUnits = 32;        // compute units of an XCD
+constexpr double kOlder = 0.15;       // by which the first workgroup's share on a unit is larger
 constexpr int32_t kWhole = 8;         // tiles of which a share holds more are not cut
 
 // The tiles of a sequence (of one key / value head).
@@ -126,12 +128,22 @@ struct TileLine {
     return q;
   }
 
+  // The shares before worker w's, in mean ones.  A compute unit issues its oldest waves first: of the
+  // workgroups on it the first placed gets a larger share, where all have one.
+  __device__ __forceinline__ double ahead(const AttnArgs& a, int32_t w) const {
+    const int32_t each = (int32_t)a.tile_groups / 8, on = (int32_t)a.tile_groups / (8 * kUnits);
+    if (workers != (int32_t)a.tile_groups || on < 2) return w;
+    const int32_t p = w % each, k = p / kUnits, r = p % kUnits;  // k have been placed on its unit before
+    const double step = 2 * kOlder / (on - 1);
+    return w - p + kUnits * (k * (1 + kOlder) - step * (k * (k - 1) / 2)) + r * (1 + kOlder - step * k);
+  }
+
   // Where worker w's share begins (the others' and w = workers: nowhere).
   __device__ __forceinline__ TileCut cut(const AttnArgs& a, int32_t w) const {
-    const TileCut none = {-1, a.n_seq + 1, 0, 0, 0, 0, 0};
+    const TileCut none = {-1, a.n_seq + 1, 0, 0, 0, 0, 0, 0, 0};
     if (w >= workers) return none;
     // (Formed by the worker that begins here and by the one that ends here, in the same way.)
-    const int64_t x = (int64_t)((double)all * ((double)w / (double)workers));
+    const int64_t x = (int64_t)((double)all * (ahead(a, w) / (double)workers));
     // Its segment, then its sequence: a sequence's tiles of all heads follow each other.
     const int L = __popcll(__ballot((incl - mine) * a.kv_heads <= x)) - 1;
     int64_t before = uniform64(__shfl(incl - mine, L, 64));
@@ -161,7 +173,8 @@ struct TileLine {
       stage = 0;
     else if (tile.stages - stage < kLeastPiece)
       stage = tile.stages;
-    return {before * a.kv_heads + head * sum + first, s, i, head, uniform(stage), tile.stages, 0};
+    return {before * a.kv_heads + head * sum + first, s, i, head, uniform(stage), tile.stages, q.start,
+            q.n, 0};
   }
 };
 
@@ -550,10 +563,11 @@ __device__ __forceinline__ void clear_rows(const AttnArgs& a, const Tile& t, int
 template <typename ET, int DP, int W, bool FULL, bool EVEN>
 __device__ __forceinline__ void tile4_share(const AttnArgs& a, uint16_t* const lds) {
   // Neighbours in the line, which read the same keys, run on the same XCD (its workgroups are those
-  // of every eighth number).
-  const int32_t each = (int32_t)a.tile_groups / 8;
-  const int32_t w = (int32_t)(blockIdx.x % 8) * each + (int32_t)(blockIdx.x / 8);
+  // of every eighth number); the workers are the first of every XCD's.
   const TileLine line(a);
+  const int32_t xcd = blockIdx.x % 8, p = blockIdx.x / 8, each = (line.workers + 7) / 8;
+  const int32_t w = p < each ? xcd * each + p
+                             : 8 * each + xcd * ((int32_t)a.tile_groups / 8 - each) + p - each;
   const TileCut from = line.cut(a, w), end = line.cut(a, w + 1);
   if (threadIdx.x == 0) a.tile_cut[w] = from;
   if (from.x < 0) return;
@@ -622,10 +636,11 @@ __global__ void __launch_bounds__(64 * kWaves, DP > 128 ? 1 : DP > 64 ? 2 : 3)
 }
 
 // One wave joins R rows of a tile's pieces side by side, from row r0 of the tile on: lanes 64 / R r
-// and on hold row r's statistics, as many pieces a turn.  Row r0 of piece k is row_of(k).
+// and on hold row r's statistics, as many pieces a turn.  Rows from `rows` on are another's.  Row r0 of
+// piece k is row_of(k).
 template <typename ET, int DP, int R, typename F>
 __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int32_t head, int32_t r0,
-                                          int32_t pieces, F&& row_of) {
+                                          int32_t pieces, int32_t rows, F&& row_of) {
   constexpr int C = DP / 64, L = 64 / R;
   const int lane = threadIdx.x & 63;
   float m = kNoMax, sum = 0.0f, acc[R][C];
@@ -633,10 +648,23 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int e = 0; e < C; ++e) acc[r][e] = 0.0f;
+  constexpr int kAhead = R == 1 ? 8 : 4;  // pieces in flight
+  float v[kAhead][R][C];
+  auto load = [&](int32_t k, int32_t end) __attribute__((always_inline)) {  // (the last again past it)
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float* const o = a.tile_o + row_of(min(k + i, end - 1)) * DP + C * lane;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[i][r][e] = o[r * DP + e];
+    }
+  };
   for (int32_t k0 = 0; k0 < pieces; k0 += L) {
     const int32_t n = min(pieces - k0, L);
     float2 st = {kNoMax, 0.0f};
     if (lane % L < n) st = a.tile_stat[row_of(k0 + lane % L) + lane / L];
+    load(k0, k0 + n);
     float top = fmaxf(m, st.x);
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
@@ -646,24 +674,15 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) part += __shfl_xor(part, d, 64);
     sum = sum * keep + part;
-    auto of_row = [&](float v, int r, int32_t k) {
-      return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), L * r + k));
+    auto of_row = [&](float x, int r, int32_t k) {
+      return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), L * r + k));
     };
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int e = 0; e < C; ++e) acc[r][e] = weighted(acc[r][e], of_row(keep, r, 0));
-    constexpr int kAhead = R == 1 ? 8 : 4;  // pieces in flight
     for (int32_t k = 0; k < n; k += kAhead) {
-      float v[kAhead][R][C];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const float* const o = a.tile_o + row_of(k0 + min(k + i, n - 1)) * DP + C * lane;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int e = 0; e < C; ++e) v[i][r][e] = o[r * DP + e];
-      }
+      if (k > 0) load(k0 + k, k0 + n);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
 #pragma unroll
@@ -676,7 +695,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int32_t row = t.row0 + r0 + r;
-    if (row >= t.rows) break;
+    if (row >= rows) break;
     const int32_t tok = (int32_t)div_by((uint32_t)row, a.group);
     const int32_t qh = head * (int32_t)a.group.d + row - tok * (int32_t)a.group.d;
     const int64_t orow = (int64_t)(t.start + tok) * a.heads + qh;
@@ -691,31 +710,38 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
 
 // Joins the pieces of the cut tiles.  A tile of n pieces is cut by n - 1 workers' beginnings; each of
 // them stands for as many workgroups, which share the tile's rows with the other beginnings'.
-constexpr int kJoinGroups = 4, kJoinThreads = 64 * kJoinWaves, kJoinEach = 4;
+constexpr int kJoinGroups = 2, kJoinThreads = 64 * kJoinWaves, kJoinEach = 4;
 template <typename ET, int DP>
 __device__ __forceinline__ void tile4_join(const AttnArgs& a) {
   const int32_t w = (int32_t)(blockIdx.x / kJoinGroups) + 1, last = (int32_t)a.tile_groups - 1;
   const int lane = threadIdx.x & 63;
   const TileCut c = a.tile_cut[w];
+  // The beginnings inside the tile: before this one, and with it and after, from the 64 around it.
+  auto around = [&](int32_t from) {
+    const int32_t k = from + lane;
+    const TileCut n = a.tile_cut[min(max(k, 0), last)];
+    return __ballot(k > 0 && k <= last && n.x == c.x && n.stage > 0 && n.stage < n.stages);
+  };
+  const uint64_t near = around(w - 32);
   if (c.x < 0 || c.stage == 0 || c.stage == c.stages) return;
-  // The beginnings inside the tile: before this one, and with it and after.
-  int32_t before = 0, after = 0;
-  for (int32_t at = w - 1;; at -= 64) {
-    const TileCut n = a.tile_cut[max(at - lane, 0)];
-    const uint64_t in = __ballot(at - lane > 0 && n.x == c.x && n.stage > 0);
-    const int32_t run = in == ~0ull ? 64 : __builtin_ctzll(~in);
-    before += run;
-    if (run < 64) break;
-  }
-  for (int32_t at = w;; at += 64) {
-    const TileCut n = a.tile_cut[min(at + lane, last)];
-    const uint64_t in = __ballot(at + lane <= last && n.x == c.x && n.stage < n.stages);
-    const int32_t run = in == ~0ull ? 64 : __builtin_ctzll(~in);
-    after += run;
-    if (run < 64) break;
-  }
+  int32_t before = (uint32_t)near == ~0u ? 32 : __builtin_clz(~(uint32_t)near);
+  if (before == 32)
+    for (int32_t at = w - 32;; at -= 64) {
+      const uint64_t in = around(at - 64);
+      const int32_t run = in == ~0ull ? 64 : __builtin_clzll(~in);
+      before += run;
+      if (run < 64) break;
+    }
+  int32_t after = (uint32_t)(near >> 32) == ~0u ? 32 : __builtin_ctz(~(uint32_t)(near >> 32));
+  if (after == 32)
+    for (int32_t at = w + 32;; at += 64) {
+      const uint64_t in = around(at);
+      const int32_t run = in == ~0ull ? 64 : __builtin_ctzll(~in);
+      after += run;
+      if (run < 64) break;
+    }
   const int32_t cuts = before + after, w0 = w - before;
-  const Tile t = tile_at(a, c.seq, seq_of<true>(a, c.seq), c.tile);
+  const Tile t = tile_at(a, c.seq, Seq{c.start, c.n, 0, 0}, c.tile);
   // The first piece is the last of worker w0 - 1's, or its only one.
   const int64_t begin = (2 * (int64_t)(w0 - 1) + (a.tile_cut[w0 - 1].x == c.x ? 0 : 1)) * kRows;
   const int64_t others = 2 * (int64_t)w0 * kRows;
@@ -724,12 +750,12 @@ __device__ __forceinline__ void tile4_join(const AttnArgs& a) {
   constexpr int32_t kAll = kJoinGroups * kJoinThreads / 64;
   const int32_t rows = min(t.rows - t.row0, kRows);
   const int32_t lo = rows * before / cuts, hi = rows * (before + 1) / cuts;
-  // Rows of the output are stored only below t.rows, but a piece's rows are all there.
+  // (A piece's rows are all there, also those that the tile does not have.)
   auto join = [&](auto EACH) {
     constexpr int R = decltype(EACH)::value;
     for (int32_t r = lo + wave * R; r < hi; r += kAll * R) {
       const int32_t r0 = min(r, kRows - R);
-      join_rows<ET, DP, R>(a, t, c.head, r0, cuts + 1, [&](int32_t k) {
+      join_rows<ET, DP, R>(a, t, c.head, r0, cuts + 1, t.row0 + hi, [&](int32_t k) {
         return r0 + (k == 0 ? begin : others + (int64_t)(k - 1) * 2 * kRows);
       });
     }

@@ -78,7 +78,8 @@ struct Read4Args {
 // of all tiles (-1: the worker has no share), and the stage of it.
 struct TileCut {
   int64_t x;
-  int32_t seq, tile, head, stage, stages, unused;
+  int32_t seq, tile, head, stage, stages;
+  int32_t start, n, unused;  // of the sequence: its first row and its tokens
 };
 
 struct AttnArgs {
