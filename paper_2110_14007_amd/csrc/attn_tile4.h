@@ -148,16 +148,25 @@ struct TileLine {
     const int L = __popcll(__ballot((incl - mine) * a.kv_heads <= x)) - 1;
     int64_t before = uniform64(__shfl(incl - mine, L, 64));
     int32_t s = uniform(L * seg);
-    Seq q;
-    Tiles t;
-    int64_t sum;
-    for (;; ++s) {
-      q = seq(a, s);
-      t = tiles_of(a, s, q);
-      sum = uniform64(t.all());
-      if (x < (before + sum) * a.kv_heads || s >= a.n_seq) break;
+    const int32_t past = min(s + seg, a.n_seq + 1);
+    while (seg > 1) {  // 64 sequences a step
+      const int32_t i = s + (int32_t)(threadIdx.x & 63);
+      const int64_t c = i < past ? tiles_of(a, i, seq_of<true>(a, i)).all() : 0;
+      const int64_t in = lane_prefix(c);
+      const int64_t sum = uniform64(__shfl(in, 63, 64));
+      if (x < (before + sum) * a.kv_heads || s + 64 >= past) {
+        const int k = __popcll(__ballot((before + in - c) * a.kv_heads <= x)) - 1;
+        before += uniform64(__shfl(in - c, k, 64));
+        s += k;
+        break;
+      }
       before += sum;
+      s += 64;
     }
+    if (s >= past) return none;
+    const Seq q = seq(a, s);
+    const Tiles t = tiles_of(a, s, q);
+    const int64_t sum = uniform64(t.all());
     if (sum == 0) return none;
     const int64_t off = x - before * a.kv_heads;
     const int32_t head = uniform(min(ratio(off, sum), a.kv_heads - 1));
@@ -538,6 +547,16 @@ struct TilePlace {
   int32_t first;  // 1: the share's first tile
 };
 
+// The next sequence after s that has tiles, 64 of them a step.
+__device__ __forceinline__ int32_t next_of(const AttnArgs& a, int32_t s) {
+  for (++s; s <= a.n_seq; s += 64) {
+    const int32_t i = s + (int32_t)(threadIdx.x & 63);
+    const uint64_t has = __ballot(i <= a.n_seq && tiles_of(a, i, seq_of<true>(a, i)).count > 0);
+    if (has) return s + __builtin_ctzll(has);
+  }
+  return s;
+}
+
 // A piece without stages, where others of its tile follow: rows of weight 0.
 template <int DP>
 __device__ __forceinline__ void clear_piece(const AttnArgs& a, int64_t row) {
@@ -602,10 +621,9 @@ __device__ __forceinline__ void tile4_share(const AttnArgs& a, uint16_t* const l
       now.tile = 0;
       if (++now.head == a.kv_heads) {
         now.head = 0;
-        do {
-          if (++now.seq > a.n_seq) return;
-          now.q = seq_of<true>(a, now.seq);
-        } while (uniform(tiles_of(a, now.seq, now.q).count) == 0);
+        now.seq = next_of(a, now.seq);
+        if (now.seq > a.n_seq) return;
+        now.q = seq_of<true>(a, now.seq);
       }
     }
   }

@@ -174,8 +174,9 @@ Plan make_plan(const tod_attn& o, int64_t tokens, int64_t n_seq, int64_t max_fre
   // The tokens' join has a workgroup of a wave a row, at most 8, for every pair.)
   constexpr int64_t kThreads = 1LL << 32;
   const int64_t join = 64 * (p.skip_rows < 8 ? p.skip_rows : 8);
+  const int64_t beside = form == Form::kPaged4 ? 2048 : 0;  // more than the tiles' workgroups
   p.fits = (!p.tile || (p.tile_slots * o.kv_heads * p.tile_parts + 1024) * 256 < kThreads) &&
-           n_seq * o.kv_heads * join < kThreads;
+           (n_seq * o.kv_heads + beside) * join < kThreads;
   p.total = at ? at : 256;
   return p;
 }

@@ -1,0 +1,654 @@
+"""How the operators around a 4-bit cache are called: one after the other as a serving step does,
+captured into a HIP graph, on other streams than the tensors', with a workspace that calls share,
+inside the workspace that they ask for, with lengths and starts that lie, without new tokens, and
+what the binding refuses.
+
+A step's results are compared with the same step over 16-bit pages that hold the values which the
+4-bit cache stands for: both are within (2.5 u + 2e-4) max|v| of the formulas (u = 2^-8 for bf16,
+2^-11 for fp16), so within twice that of each other; their log sums within 2e-4 + 2e-6 |lse|.
+"""
+import numpy as np
+import pytest
+
+from test_gpu_cache4 import U, dtype_of, f64, plain_encode, plain_rotate
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a visible MI355X"
+    from paper_2110_14007_amd import tod
+    return torch, tod
+
+
+def randn(torch, gen, *shape, dtype=None):
+    return torch.randn(*shape, generator=gen, device="cuda").to(dtype or torch.bfloat16)
+
+
+def ints(torch, values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+class Step:
+    """One serving step over a 4-bit cache with random contents: pages for the new tokens, their
+    keys and values appended, attention of their queries, and their rows read back."""
+
+    def __init__(self, torch, tod, cached, fresh, hq=4, hk=2, d=64, page=16, seed=1, name="bf16"):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.dt = dtype_of(torch, name)
+        n, self.tokens = len(cached), sum(fresh)
+        need = [-(-(c + f) // page) for c, f in zip(cached, fresh)]
+        have = [-(-c // page) for c in cached]
+        total = sum(need) + 4
+        ids = torch.randperm(total, generator=gen, device="cuda").to(torch.int32)
+        self.table = torch.full((n, max(need) + 1), -1, dtype=torch.int32, device="cuda")
+        at = 0
+        for r in range(n):
+            self.table[r, :have[r]] = ids[at:at + have[r]]
+            at += have[r]
+        self.free = ids[at:].contiguous()
+        self.cached, self.fresh = ints(torch, cached), ints(torch, fresh)
+        self.page, self.max_fresh = page, max(fresh)
+        self.q, self.k, self.v = (randn(torch, gen, self.tokens, h, d, dtype=self.dt)
+                                  for h in (hq, hk, hk))
+        self.rates = 10000.0 ** (-torch.arange(d // 2, device="cuda").float() / (d // 2))
+        self.cache = tod.Cache4.zeros(total, hk, page, d)
+        every = torch.arange(total * page, device="cuda")
+        x = randn(torch, gen, 2, total * page, hk, d, dtype=self.dt)
+        tod.tod_page_append4(x[0], x[0], x[1], every.int(), every, self.rates[:0], self.cache)
+
+    def run(self, tod, stream=None, workspace=None):
+        row_start, slot, pos, used = tod.tod_page_map(self.cached, self.fresh, self.free,
+                                                      self.table, self.page, self.tokens,
+                                                      stream=stream)
+        q = tod.tod_page_append4(self.q, self.k, self.v, pos, slot, self.rates, self.cache,
+                                 stream=stream)
+        out, lse = tod.tod_attn_paged4(q, self.cache, self.table, row_start, self.cached,
+                                       max_fresh=self.max_fresh, stream=stream,
+                                       workspace=workspace, return_lse=True)
+        k, v = tod.tod_page_read4(self.cache, slot, self.dt, stream=stream)
+        return out, lse, q, k, v, slot, pos
+
+
+CASES = {
+    "tokens": dict(cached=[100, 3, 77, 1500], fresh=[1, 1, 1, 1]),
+    "mixed": dict(cached=[100, 0, 77, 900], fresh=[1, 60, 1, 33], d=128, hq=8),
+    "chunk": dict(cached=[2000], fresh=[50], hq=8),
+    "odd_page": dict(cached=[200, 64], fresh=[40, 1], page=9, d=96, name="fp16"),
+    "wide": dict(cached=[200, 64], fresh=[40, 2], d=256, name="fp16"),
+}
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_steps_together(env, name):
+    torch, tod = env
+    s = Step(torch, tod, **CASES[name])
+    out, lse, q, k, v, slot, pos = s.run(tod)
+    kind = CASES[name].get("name", "bf16")
+    turn = (pos.cpu().numpy(), s.rates.cpu().numpy(), False)
+    size = np.abs(f64(s.q)).max()
+    assert np.abs(f64(q) - plain_rotate(f64(s.q), *turn)).max() <= (2 * U[kind] + 2.0 ** -21) * size
+    codes, scales = plain_encode(plain_rotate(f64(s.k), *turn), kind)
+    held, by = s.cache.k_codes, s.cache.k_scales
+    at, row = (slot // s.page), (slot % s.page)
+    assert np.array_equal(held[at, :, row].cpu().numpy(), codes)
+    assert np.array_equal(by[at, :, row].cpu().numpy(), scales)
+    # The same attention over 16-bit pages of the same values.
+    n = s.cache.n_pages
+    kp, vp = tod.tod_page_read4(s.cache, torch.arange(n * s.page, device="cuda"), s.dt)
+    pages = [x.view(n, s.page, s.cache.kv_heads, s.cache.dim).transpose(1, 2).contiguous()
+             for x in (kp, vp)]
+    assert torch.equal(pages[0][at, :, row], k) and torch.equal(pages[1][at, :, row], v)
+    starts = torch.nn.functional.pad(torch.cumsum(s.fresh, 0), (1, 0)).to(torch.int32)
+    want, want_lse = tod.tod_attn_paged(q, *pages, s.table, starts, s.cached, return_lse=True)
+    v_max = float(vp.abs().max())
+    assert float((out.double() - want.double()).abs().max()) <= 2 * (2.5 * U[kind] + 2e-4) * v_max
+    assert ((lse - want_lse).abs() <= 2e-4 + 2e-6 * want_lse.abs()).all()
+    # The rows go on to a detector: those of this step among the cache's own are no outliers.
+    score = tod.tod_knn_decision(v.float().flatten(1), vp.float().flatten(1), 1)
+    assert float(score.abs().max()) <= 1e-3 * v_max * s.cache.dim
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_graph_replays(env, name):
+    torch, tod = env
+    s = Step(torch, tod, **CASES[name])
+    ws = tod.Workspace()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            s.run(tod, workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = s.run(tod, workspace=ws)
+    for i in range(4):  # new contents each time, eager work and waits in between
+        gen = torch.Generator(device="cuda").manual_seed(50 + i)
+        for x in (s.q, s.k, s.v):
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+        if i % 2:  # other lengths, of as many tokens
+            s.cached -= 1
+            s.cached.clamp_(min=0)
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [x.clone() for x in got]
+        want = s.run(tod)
+        torch.cuda.synchronize()
+        for a, b in zip(replayed, want):
+            assert torch.equal(a, b)
+
+
+def test_graph_of_16_bit_appends(env):
+    torch, tod = env
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v = randn(torch, gen, 9, 4, 64), randn(torch, gen, 9, 2, 64), randn(torch, gen, 9, 2, 64)
+    kp, vp = (torch.zeros(3, 2, 16, 64, dtype=q.dtype, device="cuda") for _ in range(2))
+    slot, pos = torch.arange(9, device="cuda"), ints(torch, list(range(70, 79)))
+    rates = torch.rand(32, generator=gen, device="cuda")
+    call = lambda: tod.tod_page_append(q, k, v, pos, slot, rates, kp, vp)  # noqa: E731
+    with torch.cuda.stream(torch.cuda.Stream()):
+        call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call()
+    for i in range(4):
+        pos.add_(i)
+        slot.copy_(slot.roll(1))
+        for x in (kp, vp):
+            x.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [x.clone() for x in (out, kp, vp)]
+        for x in (kp, vp):
+            x.zero_()
+        want = (call(), kp, vp)
+        assert all(torch.equal(a, b) for a, b in zip(replayed, want))
+
+
+def test_on_another_stream(env):
+    torch, tod = env
+    s = Step(torch, tod, [100, 0, 77, 900], [1, 60, 1, 33])
+    want = [x.clone() for x in s.run(tod)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        got = s.run(tod, stream=side)  # its workspace is released while the work is under way
+        junk = [torch.full((1 << 20,), 7.0, device="cuda") for _ in range(8)]
+        side.synchronize()
+        del junk
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def queued_calls(torch, tod):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    n, hq, hk, d, page = 300, 8, 2, 64, 16
+    q, k, v = (randn(torch, gen, n, h, d) for h in (hq, hk, hk))
+    cache = tod.Cache4.zeros(300, hk, page, d)
+    slot, pos = torch.arange(n, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    rates = torch.rand(32, generator=gen, device="cuda")
+    tod.tod_page_append4(q, k, v, pos, slot, rates, cache)
+    kp, vp = (torch.zeros(300, hk, page, d, dtype=q.dtype, device="cuda") for _ in range(2))
+    table = torch.arange(300, dtype=torch.int32, device="cuda").view(1, 300)
+    starts, one, cached = ints(torch, [0, n]), ints(torch, [0, 1]), ints(torch, [4000])
+    return {
+        "append": lambda **kw: [tod.tod_page_append(q, k, v, pos, slot, rates, kp, vp, **kw)],
+        "append4": lambda **kw: [tod.tod_page_append4(q, k, v, pos, slot, rates, cache, **kw)],
+        "read4": lambda **kw: tod.tod_page_read4(cache, slot, q.dtype, **kw),
+        "chunk": lambda **kw: tod.tod_attn_paged4(q, cache, table, starts, cached, return_lse=True,
+                                                  **kw),
+        "token": lambda **kw: tod.tod_attn_paged4(q[:1], cache, table, one, cached, max_fresh=1,
+                                                  return_lse=True, **kw),
+    }
+
+
+@pytest.mark.parametrize("name", ["append", "append4", "read4", "chunk", "token"])
+def test_while_the_current_stream_is_busy(env, name):
+    torch, tod = env
+    call = queued_calls(torch, tod)[name]
+    want = [x.clone() for x in call()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    # Tensors of many sizes that the current stream fills later, freed while that is still to come.
+    sizes = [x.numel() * x.element_size() for x in want] + [1 << k for k in range(6, 26)]
+    late = [torch.empty(max(s, 1), dtype=torch.uint8, device="cuda") for s in sizes * 3]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)  # about 0.1 s
+    for x in late:
+        x.fill_(0x5a)
+    del x, late
+    got = call(stream=side)
+    side.synchronize()
+    early = [x.clone() for x in got]
+    torch.cuda.synchronize()
+    for a, b, c in zip(early, got, want):
+        assert torch.equal(b, c), "written by the current stream's work"
+        assert torch.equal(a, c)
+
+
+class Case:
+    """n new tokens of every sequence over a filled 4-bit cache."""
+
+    def __init__(self, torch, tod, seed, cached, n, hq=8, hk=2, d=128, page=32):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        cols = -(-(max(cached) + n) // page)
+        pages = len(cached) * cols
+        self.q = randn(torch, gen, n * len(cached), hq, d)
+        self.cache = tod.Cache4.zeros(pages, hk, page, d)
+        every = torch.arange(pages * page, device="cuda")
+        x = randn(torch, gen, 2, pages * page, hk, d)
+        tod.tod_page_append4(x[0], x[0], x[1], every.int(), every, torch.zeros(0, device="cuda"),
+                             self.cache)
+        self.table = torch.randperm(pages, generator=gen,
+                                    device="cuda").to(torch.int32).view(len(cached), cols)
+        self.starts = ints(torch, [n * i for i in range(len(cached) + 1)])
+        self.cached, self.n, self.tod = ints(torch, cached), n, tod
+
+    def run(self, **kw):
+        return self.tod.tod_attn_paged4(self.q, self.cache, self.table, self.starts, self.cached,
+                                        max_fresh=self.n, return_lse=True, **kw)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_two_streams_at_once(env, n):
+    torch, tod = env
+    cases = [Case(torch, tod, 1, [20000], n), Case(torch, tod, 2, [17000], n)]
+    want = [[x.clone() for x in c.run()] for c in cases]
+    ws = tod.Workspace()
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, (c, s) in enumerate(zip(cases, streams)):
+            got[i].append(c.run(workspace=ws, stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for pair in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(pair, want[i]))
+
+
+def test_graphs_that_share_a_workspace(env):
+    # Two graphs of different sizes with one workspace, replayed in turn after it has grown.
+    torch, tod = env
+    cases = [Case(torch, tod, 3, [9000], 20), Case(torch, tod, 4, [9000, 700], 60)]
+    want = [[x.clone() for x in c.run()] for c in cases]
+    large = Case(torch, tod, 5, [5000] * 6, 100)
+    ws = tod.Workspace()
+    s = torch.cuda.Stream()
+    graphs, got = [], []
+    for c in cases:
+        with torch.cuda.stream(s):
+            c.run(workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            got.append(c.run(workspace=ws))
+    with torch.cuda.stream(s):
+        large.run(workspace=ws)
+        junk = [torch.full((4 << 20,), 0x5a, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for pair in got:
+            for x in pair:
+                x.zero_()
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for pair, right in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(pair, right))
+        assert all((x == 0x5a).all() for x in junk)
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_keeps_to_its_workspace(env, name):
+    torch, tod = env
+    s = Step(torch, tod, **CASES[name])
+    want = [x.clone() for x in s.run(tod)]
+
+    class Guarded:
+        def get(self, nbytes, device):
+            self.n = nbytes
+            self.buf = torch.full((nbytes + 4096,), 0x5a, dtype=torch.uint8, device=device)
+            return self.buf[:nbytes]
+
+    ws = Guarded()
+    got = s.run(tod, workspace=ws)  # begun on 0x5a bytes: nothing in it is taken as zero
+    torch.cuda.synchronize()
+    assert (ws.buf[ws.n:] == 0x5a).all()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    with pytest.raises(tod.TodError) as e:
+        s.run(tod, workspace=tod.FixedWorkspace(256))
+    assert e.value.status == tod.TOD_ERR_WORKSPACE
+
+
+def test_outputs_and_pages_behind_the_last_row_stay(env):
+    torch, tod = env
+    guard = 4096
+    s = Step(torch, tod, [100, 0, 77], [1, 60, 1])
+    starts = ints(torch, [0, 1, 61, 62])
+    want = s.run(tod)[2].clone()
+    room = torch.full((s.q.numel() + 2 * guard,), 7.0, dtype=s.dt, device="cuda")
+    out = room[guard:-guard].view(s.q.shape)
+    got = tod.tod_attn_paged4(want, s.cache, s.table, starts, s.cached, out=out)
+    assert got.data_ptr() == out.data_ptr()
+    assert torch.equal(got, tod.tod_attn_paged4(want, s.cache, s.table, starts, s.cached))
+    before = [x.clone() for x in s.cache._tensors]
+    slot = torch.full((62,), -1, dtype=torch.int64, device="cuda")
+    tod.tod_page_append4(s.q, s.k, s.v, s.cached[:1].expand(62).contiguous(), slot, s.rates, s.cache,
+                         out=out)
+    assert all(torch.equal(a, b) for a, b in zip(before, s.cache._tensors))
+    assert (room[:guard] == 7).all() and (room[-guard:] == 7).all()
+
+
+def test_rows_past_4_gib(env):
+    # Codes past 2^32 bytes and elements past 2^33, and scales past 2^28.
+    torch, tod = env
+    page, hk, d, n_pages = 128, 8, 128, 67000
+    shape = (n_pages, hk, page)
+    k_codes, v_codes = (torch.zeros(shape + (d // 2,), dtype=torch.uint8, device="cuda")
+                        for _ in range(2))
+    k_scales, v_scales = (torch.zeros(shape + (d // 32,), dtype=torch.uint8, device="cuda")
+                          for _ in range(2))
+    assert k_codes.numel() > 1 << 32
+    cache = tod.Cache4(k_codes, k_scales, v_codes, v_scales)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n = 200
+    k, v = (randn(torch, gen, n, hk, d) for _ in range(2))
+    q = randn(torch, gen, n, 2 * hk, d)
+    pages = torch.tensor([n_pages - 1, n_pages - 3], dtype=torch.int64, device="cuda")
+    j = torch.arange(n, device="cuda")
+    slot, none = pages[j // page] * page + j % page, torch.zeros(0, device="cuda")
+    tod.tod_page_append4(q, k, v, j.int(), slot, none, cache)
+    small = tod.Cache4.zeros(2, hk, page, d)
+    tod.tod_page_append4(q, k, v, j.int(), j, none, small)
+    for a, b in zip(tod.tod_page_read4(cache, slot, k.dtype), tod.tod_page_read4(small, j, k.dtype)):
+        assert torch.equal(a, b) and float(a.abs().max()) > 1
+    for fresh in (1, 3, 40, n):
+        args = (ints(torch, [0, fresh]), ints(torch, [n - fresh]))
+        got = tod.tod_attn_paged4(q[:fresh], cache, pages.int().view(1, 2), *args, return_lse=True)
+        want = tod.tod_attn_paged4(q[:fresh], small, ints(torch, [[0, 1]]), *args, return_lse=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_16_bit_rows_past_4_gib(env):
+    torch, tod = env
+    page, hk, d, n_pages = 128, 8, 128, 33500
+    kp = torch.zeros(n_pages, hk, page, d, dtype=torch.bfloat16, device="cuda")
+    vp = torch.zeros_like(kp)
+    assert kp.numel() > 1 << 32
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n = 200
+    q, k, v = (randn(torch, gen, n, h, d) for h in (2 * hk, hk, hk))
+    j = torch.arange(n, device="cuda")
+    slot = (n_pages - 1 - j // page * 2) * page + j % page
+    out = tod.tod_page_append(q, k, v, j.int(), slot, torch.zeros(0, device="cuda"), kp, vp)
+    assert torch.equal(out, q)
+    assert torch.equal(kp[slot // page, :, slot % page], k)
+    assert torch.equal(vp[slot // page, :, slot % page], v)
+
+
+STARTS = {
+    "back_to_zero": [0, 500, 600, 0, 700],
+    "descending": [700, 600, 400, 130, 0],
+    "negative": [0, -5, 300, -(1 << 31), 700],
+    "past_the_end": [0, 1 << 30, 200, (1 << 31) - 1, 100],
+    "all_at_the_end": [700] * 150,
+    "zigzag": [(i * 389) % 701 for i in range(200)],
+    "ones_back": [i % 3 for i in range(120)],
+}
+
+
+@pytest.mark.parametrize("heads", [1, 4, 40])
+@pytest.mark.parametrize("hint", [None, 1])
+@pytest.mark.parametrize("name", sorted(STARTS))
+def test_starts_that_do_not_ascend(env, name, hint, heads):
+    """Such a call stays inside its buffers, whatever it computes, and the next with starts in order
+    is right."""
+    torch, tod = env
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    tokens, d, page, guard = 700, 64, 16, 4096
+    n = len(STARTS[name]) - 1
+    q, cols = randn(torch, gen, tokens, heads, d, dtype=torch.float16), 60
+    cache = tod.Cache4.zeros(n * cols, 1, page, d)
+    every = torch.arange(n * cols * page, device="cuda")
+    x = randn(torch, gen, 2, n * cols * page, 1, d, dtype=torch.float16)
+    tod.tod_page_append4(x[0], x[0], x[1], every.int(), every, torch.zeros(0, device="cuda"), cache)
+    table = torch.arange(n * cols, dtype=torch.int32, device="cuda").view(n, cols)
+    cached = torch.full((n,), 30, dtype=torch.int32, device="cuda")
+    room = torch.full((tokens * heads * d + 2 * guard,), 7.0, dtype=torch.float16, device="cuda")
+    out = room[guard:-guard].view(tokens, heads, d)
+
+    def run(starts, hint):
+        return tod.tod_attn_paged4(q, cache, table, ints(torch, starts), cached, out=out,
+                                   max_fresh=hint)
+
+    fine = [min(tokens, i * (tokens // n + 1)) for i in range(n + 1)]
+    want = run(fine, None).clone()
+    out.zero_()
+    run(STARTS[name], hint)
+    torch.cuda.synchronize()
+    assert (room[:guard] == 7).all() and (room[-guard:] == 7).all()
+    assert torch.isfinite(out).all()
+    assert torch.equal(run(fine, None), want)
+
+
+def test_lengths_that_lie(env):
+    # Lengths and starts out of range stay inside the buffers and leave other rows right.
+    torch, tod = env
+    for fresh in ([3, 2], [30, 20]):
+        s = Step(torch, tod, [100, 40], fresh)
+        a, t = fresh[0], sum(fresh)
+        want, want_lse, q = [x.clone() for x in s.run(tod)[:3]]
+        out, lse = tod.tod_attn_paged4(q, s.cache, s.table, ints(torch, [0, a, 1 << 30]), s.cached,
+                                       max_fresh=s.max_fresh, return_lse=True)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        starts = ints(torch, [0, a, t])
+        for wild in ((1 << 31) - 1, -(1 << 31)):
+            out = tod.tod_attn_paged4(q, s.cache, s.table, starts, ints(torch, [100, wild]))
+            assert torch.equal(out[:a], want[:a]) and torch.isfinite(out).all()
+        table = s.table.clone()
+        table[1] = (1 << 31) - 1
+        out = tod.tod_attn_paged4(q, s.cache, table, starts, s.cached)
+        assert torch.equal(out[:a], want[:a]) and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+@pytest.mark.parametrize("n_seq", [0, 1, 5])
+def test_no_new_tokens(env, n_seq, own_stream):
+    torch, tod = env
+    stream = torch.cuda.Stream() if own_stream else None
+    cache = tod.Cache4.zeros(20, 2, 8, 64)
+    for x in cache._tensors:
+        x.fill_(0x53)
+    kp, vp = (torch.full((20, 2, 8, 64), 3.0, device="cuda").half() for _ in range(2))
+    q = torch.zeros(0, 4, 64, dtype=torch.float16, device="cuda")
+    k, rates = q[:, :2].contiguous(), torch.ones(32, device="cuda")
+    slot, pos = torch.zeros(0, dtype=torch.int64, device="cuda"), ints(torch, [])
+    table = torch.arange(3 * n_seq, dtype=torch.int32, device="cuda").view(n_seq, 3)
+    starts, cached = ints(torch, [0] * (n_seq + 1)), ints(torch, [9] * n_seq)
+    torch.cuda.synchronize()
+    outs = [tod.tod_page_append4(q, k, k, pos, slot, rates, cache, stream=stream),
+            tod.tod_page_append(q, k, k, pos, slot, rates, kp, vp, stream=stream)]
+    out, lse = tod.tod_attn_paged4(q, cache, table, starts, cached, return_lse=True, stream=stream)
+    rk, rv = tod.tod_page_read4(cache, slot, torch.bfloat16, stream=stream)
+    torch.cuda.synchronize()
+    assert all(x.shape == (0, 4, 64) and x.dtype == q.dtype for x in outs + [out])
+    assert lse.shape == (0, 4) and lse.dtype == torch.float32
+    assert rk.shape == rv.shape == (0, 2, 64) and rk.dtype == torch.bfloat16
+    assert all((x == 0x53).all() for x in cache._tensors) and (kp == 3).all() and (vp == 3).all()
+
+
+def test_sequences_without_rows(env):
+    # Rows that no sequence owns are zeros; rows without any sequence are refused.
+    torch, tod = env
+    cache = tod.Cache4.zeros(4, 2, 16, 64)
+    for tokens in (3, 200):
+        q = torch.ones(tokens, 4, 64, dtype=torch.float16, device="cuda")
+        for n in (0, 2):
+            out = torch.full_like(q, 7.0)
+            args = (torch.zeros(n, 2, dtype=torch.int32, device="cuda"), ints(torch, [0] * (n + 1)),
+                    ints(torch, [5] * n))
+            if n == 0:
+                with pytest.raises(tod.TodError) as e:
+                    tod.tod_attn_paged4(q, cache, *args, out=out)
+                assert e.value.status == tod.TOD_ERR_INVALID_ARG
+                continue
+            _, lse = tod.tod_attn_paged4(q, cache, *args, out=out, return_lse=True)
+            assert (out == 0).all() and (lse == -float("inf")).all()
+
+
+def small_call(torch, tod):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    t = dict(q=randn(torch, gen, 5, 4, 64), k=randn(torch, gen, 5, 2, 64),
+             v=randn(torch, gen, 5, 2, 64), rates=torch.rand(32, generator=gen, device="cuda"),
+             kp=randn(torch, gen, 3, 2, 8, 64), vp=randn(torch, gen, 3, 2, 8, 64))
+    t["out"] = torch.empty_like(t["q"])
+    slot, pos = torch.arange(5, device="cuda"), ints(torch, [3, 1, 4, 1, 5])
+    cache = tod.Cache4.zeros(3, 2, 8, 64)
+    starts, table, cached = ints(torch, [0, 5]), ints(torch, [[2, 0]]), ints(torch, [4])
+    return t, {
+        "append": lambda t, **kw: tod.tod_page_append(
+            t["q"], t["k"], t["v"], kw.pop("pos", pos), kw.pop("slot", slot), t["rates"], t["kp"],
+            t["vp"], out=t["out"], **kw),
+        "append4": lambda t, **kw: tod.tod_page_append4(
+            t["q"], t["k"], t["v"], kw.pop("pos", pos), kw.pop("slot", slot), t["rates"],
+            kw.pop("cache", cache), out=t["out"], **kw),
+        "paged4": lambda t, **kw: tod.tod_attn_paged4(
+            t["q"], kw.pop("cache", cache), kw.pop("table", table), kw.pop("starts", starts),
+            kw.pop("cached", cached), out=t["out"], **kw),
+    }
+
+
+@pytest.mark.parametrize("name,which", [
+    ("append", "q"), ("append", "k"), ("append", "v"), ("append", "rates"), ("append", "kp"),
+    ("append", "vp"), ("append", "out"), ("append4", "q"), ("append4", "k"), ("append4", "v"),
+    ("append4", "rates"), ("append4", "out"), ("paged4", "q"), ("paged4", "out")])
+def test_refused_with_gradients(env, name, which):
+    torch, tod = env
+    tensors, calls = small_call(torch, tod)
+    want = calls[name]({n: x.clone() for n, x in tensors.items()})
+    mine = {n: x.clone() for n, x in tensors.items()}
+    mine[which].requires_grad_()
+    with pytest.raises(ValueError, match="requires a gradient"):
+        calls[name](mine)
+    with torch.no_grad():
+        got = calls[name](mine)
+    assert torch.equal(got, want)
+
+
+def test_binding_refusals(env):
+    torch, tod = env
+    t, calls = small_call(torch, tod)
+    i32, half = torch.int32, torch.float16
+    wrong = tod.Cache4.zeros(3, 2, 8, 96)
+    for name, error, change, kw in (
+            ("append", TypeError, dict(q=t["q"].float()), {}),
+            ("append", TypeError, dict(k=t["k"].to(half)), {}),
+            ("append", TypeError, dict(kp=t["kp"].to(half), vp=t["vp"].to(half)), {}),
+            ("append", TypeError, dict(rates=t["rates"].double()), {}),
+            ("append", TypeError, {}, dict(pos=torch.zeros(5, device="cuda", dtype=torch.int64))),
+            ("append", TypeError, {}, dict(slot=torch.zeros(5, device="cuda", dtype=i32))),
+            ("append", TypeError, {}, dict(slot=torch.zeros(5, dtype=torch.int64))),
+            ("append", ValueError, {}, dict(slot=torch.zeros(4, device="cuda", dtype=torch.int64))),
+            ("append", ValueError, {}, dict(pos=torch.zeros(6, device="cuda", dtype=i32))),
+            ("append", ValueError, dict(rates=torch.zeros(33, device="cuda")), {}),
+            ("append", ValueError, dict(k=t["k"][:4]), {}),
+            ("append", ValueError, dict(v=t["v"][:, :1].expand(5, 2, 64)), {}),
+            ("append", ValueError, dict(out=torch.empty_like(t["k"])), {}),
+            ("append", ValueError, dict(vp=t["vp"][:2]), {}),
+            ("append4", TypeError, dict(q=t["q"].float()), {}),
+            ("append4", ValueError, {}, dict(cache=wrong)),
+            ("append4", ValueError, dict(v=t["v"][:, :1].contiguous()), {}),
+            ("paged4", TypeError, dict(q=t["q"].float()), {}),
+            ("paged4", TypeError, {}, dict(table=torch.zeros(1, 2, device="cuda", dtype=torch.int64))),
+            ("paged4", ValueError, {}, dict(cache=wrong)),
+            ("paged4", ValueError, {}, dict(cached=ints(torch, [1, 2]))),
+            ("paged4", ValueError, {}, dict(starts=ints(torch, [0]))),
+            ("paged4", ValueError, {}, dict(scale=-1.0))):
+        with pytest.raises(error):
+            calls[name](dict(t, **change), **kw)
+    cache = tod.Cache4.zeros(3, 2, 8, 64)
+    with pytest.raises(TypeError):
+        tod.tod_page_read4(cache, torch.arange(3, device="cuda"), torch.float32)
+    with pytest.raises(TypeError):
+        tod.tod_page_read4(cache, torch.arange(3, device="cuda").int(), torch.float16)
+    with pytest.raises(ValueError):
+        tod.Cache4.zeros(3, 2, 8, 72)
+    kc, ks, vc, vs = cache._tensors
+    for bad in ((kc, vs[..., :1], vc, vs), (kc, ks, vc[:2], vs), (kc[..., :24], ks, vc[..., :24], vs)):
+        with pytest.raises((ValueError, TypeError)):
+            tod.Cache4(*bad)
+    with pytest.raises(TypeError):
+        tod.Cache4(kc.char(), ks, vc, vs)
+    # The library's own refusals come with its status.
+    wide = torch.zeros(5, 4, 68, dtype=t["q"].dtype, device="cuda")[..., :64]
+    with pytest.raises(tod.TodError) as e:  # a stride of 68 elements
+        calls["append"](dict(t, q=wide))
+    assert e.value.status == tod.TOD_ERR_UNSUPPORTED and "strides" in str(e.value)
+    with pytest.raises(tod.TodError) as e:
+        calls["append4"](dict(t, out=t["q"]))
+    assert e.value.status == tod.TOD_ERR_INVALID_ARG
+    with pytest.raises(tod.TodError) as e:
+        calls["append"](dict(t, rates=torch.zeros(0, device="cuda"), out=t["q"]))
+    assert e.value.status == tod.TOD_ERR_INVALID_ARG
+
+
+def test_views_of_one_projection(env):
+    # Queries, keys and values as a model's projection leaves them: views of one tensor.
+    torch, tod = env
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    x = randn(torch, gen, 70, 8 + 2 * 2, 64)
+    q, k, v = x[:, :8], x[:, 8:10], x[:, 10:]
+    slot, pos = torch.randperm(80, device="cuda")[:70], torch.arange(70, device="cuda").int()
+    rates = torch.rand(32, generator=gen, device="cuda")
+    caches = [tod.Cache4.zeros(5, 2, 16, 64) for _ in range(2)]
+    got = tod.tod_page_append4(q, k, v, pos, slot, rates, caches[0])
+    want = tod.tod_page_append4(q.contiguous(), k.contiguous(), v.contiguous(), pos, slot, rates,
+                                caches[1])
+    assert torch.equal(got, want)
+    assert all(torch.equal(a, b) for a, b in zip(caches[0]._tensors, caches[1]._tensors))
+
+
+def test_one_token_of_any_stride(env):
+    # torch leaves the stride of a dimension of size 1 to chance.
+    torch, tod = env
+    q = torch.randn(1, 2, 64, device="cuda").half().as_strided((1, 2, 64), (3, 64, 1))
+    k = torch.randn(1, 1, 64, device="cuda").half().as_strided((1, 1, 64), (5, 7, 1))
+    cache = tod.Cache4.zeros(1, 1, 1, 64)
+    zero = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out = tod.tod_page_append4(q, k, k, zero.int(), zero, torch.rand(32, device="cuda"), cache)
+    assert torch.equal(out, q)
+    got = tod.tod_attn_paged4(out, cache, zero.int().view(1, 1), ints(torch, [0, 1]), zero.int())
+    _, held = tod.tod_page_read4(cache, zero, torch.float16)
+    assert torch.equal(got, held.expand(1, 2, 64))
+
+
+@pytest.mark.parametrize("name,cached,fresh,hq,hk,d,page", [
+    ("many_chunks", [(37 * i) % 300 for i in range(150)], [(0, 1, 40, 3)[i % 4] for i in range(150)],
+     4, 2, 64, 16),
+    ("thousand", [(91 * i) % 200 for i in range(1000)], [1 + 20 * (i % 50 == 0) for i in range(1000)],
+     4, 1, 128, 16),
+    ("wide_groups_and_chunks", [500, 90, 1000], [1, 130, 2], 80, 2, 64, 16),
+    ("group_of_24", [500, 90, 1000], [1, 50, 2], 24, 1, 128, 24),
+    ("long_beside_short", [30000, 3, 3, 3], [17, 17, 1, 33], 8, 1, 128, 64),
+    ("d192", [700, 90], [33, 1], 4, 2, 192, 16),
+    ("d224_page_12", [700, 90], [33, 1], 4, 2, 224, 12),
+])
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+def test_batches(env, name, cached, fresh, hq, hk, d, page, kind):
+    torch, tod = env
+    s = Step(torch, tod, cached, fresh, hq=hq, hk=hk, d=d, page=page, seed=4, name=kind)
+    out, lse, q, k, v, slot, pos = s.run(tod)
+    n = s.cache.n_pages
+    kp, vp = tod.tod_page_read4(s.cache, torch.arange(n * page, device="cuda"), s.dt)
+    pages = [x.view(n, page, hk, d).transpose(1, 2).contiguous() for x in (kp, vp)]
+    starts = torch.nn.functional.pad(torch.cumsum(s.fresh, 0), (1, 0)).to(torch.int32)
+    want, want_lse = tod.tod_attn_paged(q, *pages, s.table, starts, s.cached, return_lse=True)
+    v_max = float(vp.abs().max())
+    assert float((out.double() - want.double()).abs().max()) <= 2 * (2.5 * U[kind] + 2e-4) * v_max
+    assert ((lse - want_lse).abs() <= 2e-4 + 2e-6 * want_lse.abs()).all()
