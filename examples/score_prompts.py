@@ -6,12 +6,15 @@ a first batch.  The rows that the detector scores come out of the sequence opera
 
   tod_attn_prompt   whole packed prompts (the fitting batch)
   tod_page_map      pages and slots of a step's new tokens from the requests' lengths
-  tod_page_write    their keys and values into the pages
+  tod_page_append   their queries and keys rotated by position, keys and values into the pages
   tod_attn_paged    chunks of new prompts and single tokens over the pages
   tod_knn_decision  the scores of the new requests
 
+With --four the cache holds 4-bit rows, a quarter of the memory: tod_page_append4 and
+tod_attn_paged4.
+
 Usual prompts draw their tokens from a small part of the vocabulary, odd ones from the rest.
-Run: python examples/score_prompts.py
+Run: python examples/score_prompts.py [--four]
 """
 import os
 import sys
@@ -52,14 +55,15 @@ class Decoder:
         lo, hi = x.float().chunk(2, -1)
         return torch.cat([lo * a.cos() - hi * a.sin(), lo * a.sin() + hi * a.cos()], -1).half()
 
-    def forward(self, tokens, pos, attend):
-        """Hidden states [tokens, width]; attend(layer, q, k, v) -> [tokens, heads, dim]."""
+    def forward(self, tokens, attend):
+        """Hidden states [tokens, width]; attend(layer, q, k, v) -> [tokens, heads, dim] rotates
+        queries and keys by position."""
         x = self.embed[tokens]
         h, g, d = self.heads, self.kv_heads, self.dim
         for i in range(self.layers):
             qkv = (self.norm(x) @ self.qkv[i]).view(-1, h + 2 * g, d)
-            q, k = self.rotate(qkv[:, :h], pos), self.rotate(qkv[:, h:h + g], pos)
-            x = x + attend(i, q, k, qkv[:, h + g:]).reshape(x.shape) @ self.proj[i]
+            o = attend(i, qkv[:, :h], qkv[:, h:h + g], qkv[:, h + g:])
+            x = x + o.reshape(x.shape) @ self.proj[i]
             x = x + torch.nn.functional.gelu(self.norm(x) @ self.up[i]) @ self.down[i]
         return self.norm(x)
 
@@ -70,8 +74,8 @@ def whole_prompts(model, prompts):
     row_start = torch.nn.functional.pad(torch.cumsum(lens, 0), (1, 0)).to(torch.int32)
     pos = torch.cat([torch.arange(len(p), device="cuda") for p in prompts])
     ws = tod.Workspace()
-    h = model.forward(torch.cat(prompts), pos, lambda i, q, k, v: tod.tod_attn_prompt(
-        q, k, v, row_start, workspace=ws))
+    h = model.forward(torch.cat(prompts), lambda i, q, k, v: tod.tod_attn_prompt(
+        model.rotate(q, pos), model.rotate(k, pos), v, row_start, workspace=ws))
     return sums_of(h, lens) / lens[:, None]
 
 
@@ -83,16 +87,20 @@ def sums_of(h, lens):
 
 
 class Server:
-    """Requests over a paged cache, served in steps that mix chunks of prompts and single tokens."""
+    """Requests over a paged cache, of 4-bit rows with `four`, served in steps that mix chunks of
+    prompts and single tokens."""
 
-    def __init__(self, model, prompts, page=16, chunk=48):
+    def __init__(self, model, prompts, page=16, chunk=48, four=False):
         self.model, self.prompts, self.page, self.chunk = model, prompts, page, chunk
         n, cols = len(prompts), max(-(-len(p) // page) for p in prompts)
         pages = sum(-(-len(p) // page) for p in prompts)
         shape = (pages, model.kv_heads, page, model.dim)
-        self.k_pages = [torch.zeros(shape, dtype=torch.float16, device="cuda")
-                        for _ in range(model.layers)]
-        self.v_pages = [torch.zeros_like(p) for p in self.k_pages]
+        self.four = four
+        if four:
+            self.caches = [tod.Cache4.zeros(*shape) for _ in range(model.layers)]
+        else:
+            self.caches = [[torch.zeros(shape, dtype=torch.float16, device="cuda")
+                            for _ in range(2)] for _ in range(model.layers)]
         self.table = torch.full((n, cols), -1, dtype=torch.int32, device="cuda")
         self.free = torch.randperm(pages, device="cuda").to(torch.int32)
         self.done = [0] * n
@@ -112,11 +120,15 @@ class Server:
                                                       self.page, sum(fresh))
 
         def attend(i, q, k, v):
-            tod.tod_page_write(k, v, slot, self.k_pages[i], self.v_pages[i])
-            return tod.tod_attn_paged(q, self.k_pages[i], self.v_pages[i], self.table, row_start,
-                                      cached, max_fresh=max(fresh), workspace=self.ws)
+            cache, where = self.caches[i], (self.table, row_start, cached)
+            if self.four:
+                q = tod.tod_page_append4(q, k, v, pos, slot, self.model.rates, cache)
+                return tod.tod_attn_paged4(q, cache, *where, max_fresh=max(fresh),
+                                           workspace=self.ws)
+            q = tod.tod_page_append(q, k, v, pos, slot, self.model.rates, *cache)
+            return tod.tod_attn_paged(q, *cache, *where, max_fresh=max(fresh), workspace=self.ws)
 
-        h = self.model.forward(tokens, pos, attend)
+        h = self.model.forward(tokens, attend)
         taken, lacking = used.tolist()
         if lacking:
             raise RuntimeError("the cache has no page left for %d tokens" % lacking)
@@ -135,11 +147,11 @@ def make_prompts(n, lo, hi, seed, part):
     return [torch.randint(part[0], part[1], (m,), generator=gen, device="cuda") for m in lens]
 
 
-def main():
+def main(four=False):
     model = Decoder()
     fitted = whole_prompts(model, make_prompts(200, 80, 200, 1, (0, 64)))
     usual, odd = make_prompts(24, 80, 200, 2, (0, 64)), make_prompts(6, 80, 200, 3, (64, 512))
-    server = Server(model, usual + odd)
+    server = Server(model, usual + odd, four=four)
     steps = 0
     while server.step():
         steps += 1
@@ -153,4 +165,4 @@ def main():
 
 
 if __name__ == "__main__":
-    main()
+    main(four="--four" in sys.argv[1:])

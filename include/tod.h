@@ -603,8 +603,9 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
  * = r elements of a head, the pairs (x_i, x_{i + r/2}), or with `interleaved`
  * (x_2i, x_2i+1), i < r / 2, turn by the angle t = pos * rates[i]:
  *   (x, y) -> (x cos t - y sin t, x sin t + y cos t)
- * The angle and its cosine and sine are formed in 64 bits (the product is exact
- * below 2^53).  Values and the elements from r on are not rotated.
+ * The angle is formed and reduced to a quarter turn in 64 bits (the product is exact
+ * below 2^53), however far the position.  Values and the elements from r on are not
+ * rotated.
  */
 typedef struct {
   uint32_t struct_size; /* must be sizeof(tod_append) */
@@ -630,7 +631,9 @@ void tod_default_append(tod_append* append, int32_t heads, int32_t kv_heads, int
  *                 rotary is 0
  *   slot, k_pages, v_pages: as in tod_page_write
  *   q_out [tokens, heads, dim] contiguous, sharing no memory with q, k or v
- * Rotated elements are fp32 sums of two products, rounded once.
+ * Rotated elements are fp32 sums of two products with an fp32 cosine and sine, then
+ * rounded to the type.  Of a slot that several tokens share, parts of the row may come
+ * from different ones.
  */
 tod_status tod_page_append(const tod_append* append, const void* q, const void* k, const void* v,
                            int64_t tokens, const int32_t* pos, const float* rates,

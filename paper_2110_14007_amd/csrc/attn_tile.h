@@ -30,11 +30,6 @@ constexpr int kRows = 32 * kWaves;  // rows of a workgroup
 constexpr int kKeys = 32;           // keys of a stage
 constexpr int kRing = 4;            // stages of K, and of V, in LDS
 constexpr uint32_t kNoLoad = ~0u;   // offset of a lane that loads nothing
-// Growth of the maximum (log2) that m may lag behind.  With kBias the weights stay below 2^15.5 in
-// fp16, whose numbers end at 2^16, and at 1 at most in bf16.  (512 tokens after 60,007, 2 heads of
-// 128, fp16: 287 us, without a bias 280.)
-template <typename ET>
-constexpr float kSlack = std::is_same<ET, _Float16>::value ? 5.5f : 8.0f;
 
 // What a workgroup works on.
 struct Tile : Seq {

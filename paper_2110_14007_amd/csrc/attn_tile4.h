@@ -1,18 +1,35 @@
-// Attention tiles over a 4-bit cache: the work of attn_tile.h, dealt to as many
-// workgroups as fit on the GPU at once.
+// Attention tiles over a 4-bit cache: the steps of attn_tile.h (S^T = K Q^T, the
+// softmax in a lane, P from the accumulators, three products' work in slots of
+// one MFMA), with stages that are converted on the way.  A wave loads its eight
+// rows of a stage's codes into registers a turn ahead and writes their values to
+// LDS between the products, word by word: conversions and LDS writes then fill
+// slots that the matrix pipe leaves.  Bound by the products and by the vector
+// instructions beside them, as over 16-bit pages.
 //
 // The tiles of all sequences and key / value heads form one line, each as long
-// as the keys that it sees and a constant for its start and its stores.  A
-// worker takes an equal share of that line, wherever it begins and ends: chunks
-// of prompts over caches of any lengths beside each other leave no worker
-// waiting for the longest, and a single chunk is shared by all.  At most the
-// first and the last tile of a share are cut; of those a worker leaves (m, sum, O)
-// and a second kernel joins the pieces.  A tile that is short beside a share is
-// not cut: the cut moves to its nearer end.
+// as the keys that it sees and a constant for its start and its stores, and as
+// many workgroups as fit on the GPU at once take shares of it, wherever those
+// begin and end: chunks of prompts over caches of any lengths beside each
+// other leave no worker waiting for the longest, and a single chunk is shared by
+// all.  At most the first and the last tile of a share are cut; of those a
+// worker leaves (m, sum, O) and a second kernel joins the pieces.
 //
 // The lengths are known on the device only.  Tile i of a sequence weighs
 // base + step (i + 1), so that the line's sums have a closed form: the worker
 // finds its place in it by the sequences' sums, one segment a lane, and a root.
+//
+// Sequences of few rows are the token workers' of attn_token4.h, which here are
+// the tiles' waves: half of the workgroups begin with them, half end with them, so
+// that the memory is read while products are formed.
+//
+// Measured, rows of 128, whole calls: a chunk of 512 after 60,007, 16 / 2 heads, fp16
+// 298 us (864 TFLOP/s); 12 prompts of 90 to 2,500, 32 / 8 heads 325 us; a prompt of
+// 8,000 585 us (895 TFLOP/s); 4 chunks and 40 tokens 214 us.  Steps on the way: tiles in
+// a grid with the keys of all split alike, as over 16-bit pages, 308 us for those 4
+// chunks and 40 tokens, dealt 255; tokens in a launch of their own 235, in this one 223.
+// Conversions in front of the products instead of between them: 338 us for the chunk, where
+// this took 316.  8 chunks of 300 to 600, rows of 64: 230 us with three workgroups a unit, 256
+// with two.
 #pragma once
 
 #include "attn_tile.h"
@@ -21,12 +38,21 @@
 namespace tod {
 namespace attn {
 
-constexpr int32_t kTileWeight = 256;  // of a tile's start and stores, in keys
-constexpr int32_t kShareKeys = 512;   // least weight of a worker's share, where there are few tiles
-constexpr int32_t kLeastPiece = 4;    // stages that a cut leaves on either side
-constexpr int32_t kUnits = 32;        // compute units of an XCD
-constexpr double kOlder = 0.15;       // by which the first workgroup's share on a unit is larger
-constexpr int32_t kWhole = 8;         // tiles of which a share holds more are not cut
+// Of a tile's start and stores, in keys.  (12 prompts of 90 to 2,500: 343 us with 256, 388 with 128,
+// 353 with 384, 378 with 640.)
+constexpr int32_t kTileWeight = 256;
+// Least weight of a worker's share, where there are few tiles.  (60 tokens after 500, 32 / 8 heads:
+// 27 us with 128, 28 with 64, 33 with 32, 37 with 512; a prompt of 300: 30, 35, 35 and 36.)
+constexpr int32_t kShareKeys = 128;
+// Stages that a cut leaves on either side, else it moves to the tile's end: a piece has its partial
+// results to store and to join.  (A prompt of 300 25 us with 6, 30 with 4; 100 prompts of 100 to 200
+// 124 us with 4 to 16, 141 with 1; 6 chunks and 54 tokens 140 us, 147 with 12.)
+constexpr int32_t kLeastPiece = 6;
+constexpr int32_t kUnits = 32;  // compute units of an XCD
+// By which the share of a unit's first workgroup is larger.  (12 prompts 325 us with 0.15, 339 with 0,
+// 330 with 0.2; a chunk of 512 after 60,007 298, 309 and 301; one of 64 after 30,000, whose shares are
+// short, 72 and 68 with 0.)
+constexpr double kOlder = 0.15;
 
 // The tiles of a sequence (of one key / value head).
 struct Tiles {
@@ -176,9 +202,7 @@ struct TileLine {
     const Tile tile = tile_at(a, s, q, i);
     int32_t stage = (int32_t)((double)tile.stages * (double)(y - first) / (double)weight);
     stage = min(max(stage, 0), tile.stages);
-    if (weight * kWhole * workers < all)
-      stage = 2 * stage < tile.stages ? 0 : tile.stages;
-    else if (stage < kLeastPiece)
+    if (stage < kLeastPiece)
       stage = 0;
     else if (tile.stages - stage < kLeastPiece)
       stage = tile.stages;
@@ -205,10 +229,10 @@ __device__ __forceinline__ int swizzle_v4(int row) {
   return DP == 64 ? 0 : (row & 3) << 1 | (row & 1);
 }
 
-// A workgroup's work on `count` stages, at least one, of a tile from jb on: the tile's output, or partial results into
-// the rows from part_row on where that is not below 0.  W: the elements of a row that the products
-// take, of the DP that its stages have room for.  FULL: the rows have DP elements.  EVEN: pages hold
-// whole groups of eight rows.
+// A workgroup's work on `count` stages, at least one, of a tile from jb on: the tile's output, or
+// partial results into the rows from part_row on where that is not below 0.  W: the elements of a row
+// that the products take, of the DP that its stages have room for.  FULL: the rows have DP elements.
+// EVEN: pages hold whole groups of eight rows.
 template <typename ET, int DP, int W, bool FULL, bool EVEN>
 __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given, uint32_t head,
                                            int32_t jb, int32_t count, const int64_t part_row,
@@ -727,7 +751,9 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const Tile& t, int3
 }
 
 // Joins the pieces of the cut tiles.  A tile of n pieces is cut by n - 1 workers' beginnings; each of
-// them stands for as many workgroups, which share the tile's rows with the other beginnings'.
+// them stands for kJoinGroups workgroups, which share the tile's rows with the other beginnings'.
+// (Bound by the chain of loads: 16 to 19 us for 512 workers in 1,022 workgroups, which are all there at
+// once, 20 to 25 with four for every beginning.)
 constexpr int kJoinGroups = 2, kJoinThreads = 64 * kJoinWaves, kJoinEach = 4;
 template <typename ET, int DP>
 __device__ __forceinline__ void tile4_join(const AttnArgs& a) {

@@ -79,7 +79,8 @@ struct Read4Args {
 struct TileCut {
   int64_t x;
   int32_t seq, tile, head, stage, stages;
-  int32_t start, n, unused;  // of the sequence: its first row and its tokens
+  int32_t start, n;  // of the sequence: its first row and its tokens
+  int32_t padding;
 };
 
 struct AttnArgs {
@@ -110,7 +111,7 @@ struct AttnArgs {
   // A 4-bit cache: its codes are k and v.
   const uint8_t *k_scales, *v_scales;
   TileCut* tile_cut;  // [workers]; each has two tiles' rows in tile_stat and tile_o
-  int32_t ride, unused;  // 1: the tiles' waves are the token workers too
+  int32_t ride;       // 1: the tiles' waves are the token workers too
 };
 
 // Packed rows that the token kernel takes: a product's 32 columns.  (96 tokens over caches of 100
@@ -121,7 +122,8 @@ constexpr int kTokenMaxRows = 32;
 // TB/s with four a unit, 5.3 with five, which do not all stay resident, 6.0 with eight of 16 KiB.)
 constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 
-// Workers of the tiles over a 4-bit cache: as many workgroups as fit on 256 compute units at once.
+// Workers of the tiles over a 4-bit cache: as many workgroups as fit on 256 compute units at once, by
+// LDS and registers.
 constexpr int32_t tile4_workers(int32_t dim) { return dim > 128 ? 256 : dim > 64 ? 512 : 768; }
 // Over a 4-bit cache: three waves on each of 1,024 SIMDs, two for more than 128 elements.
 constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 2048 : 3072; }

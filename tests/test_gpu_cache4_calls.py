@@ -652,3 +652,11 @@ def test_batches(env, name, cached, fresh, hq, hk, d, page, kind):
     v_max = float(vp.abs().max())
     assert float((out.double() - want.double()).abs().max()) <= 2 * (2.5 * U[kind] + 2e-4) * v_max
     assert ((lse - want_lse).abs() <= 2e-4 + 2e-6 * want_lse.abs()).all()
+
+
+def test_example(env):
+    torch, _ = env
+    from examples import score_prompts
+    score, drift = score_prompts.main(four=True)
+    assert score.shape == (30,) and bool(torch.isfinite(score).all())
+    assert drift > 0
