@@ -222,6 +222,9 @@ struct Codes {
 
 constexpr int kRing4 = 2;  // stages of K, and of V, in LDS
 
+// A wave's rows of a page that does not exist.
+static __device__ const uint4 kZeroRows[64] = {};
+
 // Pieces of V rows: as swizzle_v for the transposing read; that neighbouring rows differ in the lowest
 // bit too puts a wave's writes, every other piece of two rows at a time, on different banks.
 template <int DP>
@@ -300,9 +303,12 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
     const uint8_t* c = (const uint8_t*)(isk ? a.k : a.v);
     const uint8_t* b = isk ? a.k_scales : a.v_scales;
     if constexpr (EVEN) {
-      const uint64_t r = row == ~0u ? 0 : row;  // (cleared when they are put)
-      to.words = load_global<typename Codes<DP>::W>(c + r * row_bytes + code_at);
-      to.scale = load_global<uint32_t>(b + r * row_scales + (scale_at & ~3u));
+      const uint64_t r = row;
+      const uint8_t* const zeros = (const uint8_t*)kZeroRows;
+      c = row == ~0u ? zeros : c + r * row_bytes;
+      b = row == ~0u ? zeros : b + r * row_scales;
+      to.words = load_global<typename Codes<DP>::W>(c + code_at);
+      to.scale = load_global<uint32_t>(b + (scale_at & ~3u));
     } else {
       const bool ok = row != ~0u;
       const uint8_t* const zeros = (const uint8_t*)&kZeros;
@@ -310,25 +316,18 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
       to.scale = load_global<uint8_t>(ok ? b + (uint64_t)row * row_scales + in4 / 32 : zeros);
     }
   };
-  // Word x of stage i's codes, found in `row`.  A value that does not exist may not meet a weight, not
-  // even one of 0.
-  auto put = [&](auto ISK, int x, int32_t i, uint32_t row, int ring, const Codes<DP>& from)
+  // Word x of stage i's codes.  A row that does not exist may hold values that are not finite, which
+  // may not meet a weight, not even one of 0: it gets the least scale.
+  auto put = [&](auto ISK, int x, int32_t i, int ring, const Codes<DP>& from)
       __attribute__((always_inline)) {
     constexpr bool isk = decltype(ISK)::value;
     if (!FULL && e4 >= a.dim) return;
     uint16_t* const to = lds + kStage * (ring + (isk ? 0 : kRing4)) + row4 * DP;
     const int swizzle = isk ? swizzle_k<DP>(row4) : swizzle_v4<DP>(row4);
-    uint32_t w = from.words[x];
-    float scale;
-    if constexpr (EVEN) {
-      w &= row == ~0u ? 0u : ~0u;
-      if (!isk && (jb + i + 1) * kKeys > t.seen)
-        w &= (jb + i) * kKeys + row4 < t.seen ? ~0u : 0u;
-      scale = scale_of(from.scale >> (8 * (scale_at & 3)) & 0xff);
-    } else {
-      scale = scale_of(from.scale);
-    }
-    *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) = eight_values<ET>(w, scale);
+    uint32_t s = EVEN ? scale_among(from.scale, scale_at & 3) : from.scale << 23;
+    if (EVEN && !isk) s = (jb + i) * kKeys + row4 < t.seen ? s : 0;
+    *(u32x4*)(to + 8 * ((e4 / 8 + x) ^ swizzle)) =
+        eight_values<ET>(from.words[x], __uint_as_float(s));
   };
   constexpr std::true_type kIsK{};
   constexpr std::false_type kIsV{};
@@ -474,8 +473,9 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
   u32x4 pa[2], pb[2];
   pb[0] = pb[1] = u32x4{0, 0, 0, 0};
   Codes<DP> kcodes, vcodes;  // of K j + 2 and V j, from the turn before
-  uint32_t r0 = find(0), r1 = find(1), r2 = find(2);  // rows of stages j, j + 1 and j + 2
+  uint32_t r1 = find(1), r2 = find(2);  // rows of stages j + 1 and j + 2
   {
+    const uint32_t r0 = find(0);
     Codes<DP> k0, k1;
     fetch(kIsK, r0, k0);
     fetch(kIsK, r1, k1);
@@ -483,8 +483,8 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
     fetch(kIsV, r0, vcodes);
 #pragma unroll
     for (int x = 0; x < DP / 64; ++x) {
-      put(kIsK, x, 0, r0, 0, k0);
-      put(kIsK, x, 1, r1, 1, k1);
+      put(kIsK, x, 0, 0, k0);
+      put(kIsK, x, 1, 1, k1);
     }
     mt::stage_barrier();
   }
@@ -498,7 +498,7 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
     if (j > open) clear(j - 1);
     // K j + 2 and V j go to LDS word by word, then the loads of those after them begin.
     constexpr int kWords = DP / 64, kFirst = kCheck + 1, kLast = kSlots - 2;
-    uint32_t next = 0;
+    const uint32_t next = find(j + 3);  // (here, for it branches)
     step((jb + j) * kKeys, (1 - r) * kS, (1 - r) * kS, s, n, p, pn,
          [&](auto I) __attribute__((always_inline)) {
            constexpr int i = decltype(I)::value;
@@ -506,18 +506,16 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
              constexpr int x = decltype(X)::value;
              if constexpr (i == kFirst + (DP > 128 ? 0 : x * (kLast - kFirst) / (2 * kWords))) {
                if constexpr (x < kWords)
-                 put(kIsK, x, j + 2, r2, r, kcodes);
+                 put(kIsK, x, j + 2, r, kcodes);
                else
-                 put(kIsV, x - kWords, j, r0, r, vcodes);
+                 put(kIsV, x - kWords, j, r, vcodes);
              }
            });
-           if constexpr (i == kLast) next = find(j + 3);
            if constexpr (i == kSlots - 1) {
              fetch(kIsK, next, kcodes);
              fetch(kIsV, r1, vcodes);
            }
          });
-    r0 = r1;
     r1 = r2;
     r2 = next;
   };
