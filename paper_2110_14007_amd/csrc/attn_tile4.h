@@ -3,8 +3,9 @@
 // one MFMA), with stages that are converted on the way.  A wave loads its eight
 // rows of a stage's codes into registers a turn ahead and writes their values to
 // LDS between the products, word by word: conversions and LDS writes then fill
-// slots that the matrix pipe leaves.  Bound by the products and by the vector
-// instructions beside them, as over 16-bit pages.
+// slots that the matrix pipe leaves.  Bound by the products and what is issued
+// beside them, as over 16-bit pages: fewer vector instructions or other orders changed
+// the time by 1% at most, and cards differ by 10 by their clocks.
 //
 // The tiles of all sequences and key / value heads form one line, each as long
 // as the keys that it sees and a constant for its start and its stores, and as
@@ -23,13 +24,14 @@
 // that the memory is read while products are formed.
 //
 // Measured, rows of 128, whole calls: a chunk of 512 after 60,007, 16 / 2 heads, fp16
-// 298 us (864 TFLOP/s); 12 prompts of 90 to 2,500, 32 / 8 heads 325 us; a prompt of
-// 8,000 585 us (895 TFLOP/s); 4 chunks and 40 tokens 214 us.  Steps on the way: tiles in
+// 284 us (910 TFLOP/s); 12 prompts of 90 to 2,500, 32 / 8 heads 310 us; a prompt of
+// 8,000 558 us (940 TFLOP/s); 4 chunks and 40 tokens 203 us.  Steps on the way: tiles in
 // a grid with the keys of all split alike, as over 16-bit pages, 308 us for those 4
 // chunks and 40 tokens, dealt 255; tokens in a launch of their own 235, in this one 223.
 // Conversions in front of the products instead of between them: 338 us for the chunk, where
-// this took 316.  8 chunks of 300 to 600, rows of 64: 230 us with three workgroups a unit, 256
-// with two.
+// this took 316; pages found between the products, whose branches moved the exponentials
+// behind them, 297 and 284.  8 chunks of 300 to 600, rows of 64: 230 us with three
+// workgroups a unit, 256 with two.
 #pragma once
 
 #include "attn_tile.h"
@@ -376,7 +378,7 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
   // 32 (n; at kat in the K ring) and the product of the 32 before (weights p; at vat in the V
   // ring).  The three do not depend on each other.  They are laid out in slots of one MFMA, the
   // LDS reads of the MFMA kAhead slots on, a share of the exponentials, and of the staging.
-  constexpr int kSlots = KC + 2 * DB, kAhead = DP > 128 ? 2 : 4, kCheck = 2;
+  constexpr int kSlots = KC + 2 * DB, kAhead = DP > 128 ? 2 : 3, kCheck = 2;
   auto step = [&](int32_t j0, int kat, int vat, f32x16& s, f32x16& n, const u32x4 (&p0)[2],
                   u32x4 (&pn)[2], auto&& staging) __attribute__((always_inline)) {
     u32x4 p[2] = {p0[0], p0[1]};
@@ -496,7 +498,8 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
                   u32x4 (&pn)[2]) __attribute__((always_inline)) {  // r: j % 2
     mt::stage_barrier();
     if (j > open) clear(j - 1);
-    // K j + 2 and V j go to LDS word by word, then the loads of those after them begin.
+    // K j + 2 and V j go to LDS word by word; the loads of those after them begin as soon as their
+    // registers are free.
     constexpr int kWords = DP / 64, kFirst = kCheck + 1, kLast = kSlots - 2;
     const uint32_t next = find(j + 3);  // (here, for it branches)
     step((jb + j) * kKeys, (1 - r) * kS, (1 - r) * kS, s, n, p, pn,
@@ -509,12 +512,10 @@ __device__ __forceinline__ void tile4_work(const AttnArgs& a, const Tile& given,
                  put(kIsK, x, j + 2, r, kcodes);
                else
                  put(kIsV, x - kWords, j, r, vcodes);
+               if constexpr (x == kWords - 1) fetch(kIsK, next, kcodes);
+               if constexpr (x == 2 * kWords - 1) fetch(kIsV, r1, vcodes);
              }
            });
-           if constexpr (i == kSlots - 1) {
-             fetch(kIsK, next, kcodes);
-             fetch(kIsV, r1, vcodes);
-           }
          });
     r1 = r2;
     r2 = next;

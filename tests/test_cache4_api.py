@@ -238,3 +238,12 @@ def test_binding_refuses_host_tensors(tod):
             call()
     with pytest.raises(ValueError):
         tod.Cache4.zeros(2, 2, 16, 40, device="cpu")
+
+
+def test_most_sequences(tod):
+    # The join has 512 threads for every sequence and key / value head, beside the tiles' own.
+    def room(n):
+        return tod.tod_attn_paged4_workspace_size(8, 1, 64, 100, n, 100)
+
+    assert room(8_000_000) > 0
+    assert room((1 << 23) - 1000) == 0 and room(1 << 23) == 0

@@ -1,9 +1,10 @@
 """The rotating appends and the 4-bit cache on the GPU against plain implementations in 64 bits.
 
-Tolerances, derived.  Rotated 16-bit rows: x cos - y sin with cos and sin right to 2^-24 of
-themselves, one product rounded, the sum rounded once (2^-24 each): off by at most
-2^-24 (3 |x| + 3 |y|), then rounded to the type: half a step of the value, and half of its smallest step.
-The tests allow u |want| + 2^-22 (|x| + |y|) + tiny.  What a 4-bit cache holds is compared for
+Tolerances, derived.  Rotated 16-bit rows: x cos - y sin with cos and sin right to 2^-23 (the angle
+is reduced in 64 bits and rounded to 32, the series is one of 32 bits), products and their sum rounded
+(2^-24 each): off by at most 2^-22 (|x| + |y|), then rounded to the type: half a step of the value, and
+half of its smallest step.  With no element larger than m the tests allow u |want| + 2^-21 m + tiny.
+What a 4-bit cache holds is compared for
 equality: scales and codes come from 64-bit arithmetic, and of the few thousand blocks here none lies
 within 2^-50 of a border but those that lie on it exactly.
 
