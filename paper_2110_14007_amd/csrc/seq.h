@@ -126,7 +126,7 @@ constexpr int64_t token_workers(int32_t dim) { return dim > 128 ? 512 : 1024; }
 // LDS and registers.
 constexpr int32_t tile4_workers(int32_t dim) { return dim > 128 ? 256 : dim > 64 ? 512 : 768; }
 // Over a 4-bit cache: three waves on each of 1,024 SIMDs, two for more than 128 elements.
-constexpr int64_t token4_workers(int32_t dim) { return dim > 128 ? 2048 : 3072; }
+constexpr int64_t token4_workers(int32_t dim) { return (dim > 128 ? 2 : 3) * 1024; }
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
 hipError_t launch_page_write(const PageWriteArgs& a, hipStream_t s);

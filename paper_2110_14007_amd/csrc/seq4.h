@@ -15,11 +15,6 @@ namespace tod {
 // A float with the scale's exponent (the conversions read nothing else of it).
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// The bits of such a float, of byte `at` of a word of scales.
-__device__ __forceinline__ uint32_t scale_among(uint32_t word, uint32_t at) {
-  return __builtin_amdgcn_alignbit(word, word, 9 + 8 * at);
-}
-
 // The two values of byte SEL of `codes`, as 16-bit elements.
 template <typename ET, int SEL>
 __device__ __forceinline__ uint32_t two_values(uint32_t codes, float scale) {
