@@ -13,8 +13,8 @@
 // the smallest with a <= 7 2^e: then the largest error is 2^e, at 7 and
 // between 4 and 6 alike.  e stays in [-23, 13] (fp16) or [-125, 125] (bf16), so
 // that every value that a code and a scale stand for is a number of the type.
-// Keys are rotated in 64 bits and compared with the borders of scales and codes
-// as what they are there: an element next to a border gets the code that the
+// Keys are rotated in 64 bits and rounded to odd 32-bit numbers, which no border
+// of scales and codes is: an element next to a border gets the code that the
 // formula gives.
 //
 // All three are bound by their bytes, or by their start where there are few.
@@ -152,13 +152,14 @@ __device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
   return w;
 }
 
-// y as a float on the same side of every float that y is: what y rounds to, or its neighbour towards y.
-// Borders of codes and of scales are floats, so that comparisons with them come out as y's do.
-__device__ __forceinline__ float beside(double y) {
+// y rounded to a float to odd: exact, or the one of its two neighbours whose last bit is set.  Floats
+// whose last bit is clear, the borders of codes and of scales among them, then lie on the same side of
+// the result as of y, and are met by no other y than themselves.
+__device__ __forceinline__ float to_odd(double y) {
   const float f = (float)y;
   const uint32_t u = __float_as_uint(f);
   const double back = (double)f;
-  return __uint_as_float(back == y ? u : fabs(y) > fabs(back) ? u + 1 : u - 1);
+  return __uint_as_float((fabs(back) > fabs(y) ? u - 1 : u) | (back != y ? 1u : 0u));
 }
 
 // Exponent of the scale of a block whose largest magnitude is a (finite), from a's bits: from
@@ -185,7 +186,7 @@ __device__ __forceinline__ uint32_t encode(const double (&x)[8], uint32_t* scale
   uint32_t top = 0;  // magnitudes compare as their bits
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    f[i] = beside(x[i]);
+    f[i] = to_odd(x[i]);
     top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
   }
   top = over_block(top);
