@@ -603,9 +603,9 @@ tod_status tod_attn_paged(const tod_attn* attn, const void* q, const void* k_pag
  * = r elements of a head, the pairs (x_i, x_{i + r/2}), or with `interleaved`
  * (x_2i, x_2i+1), i < r / 2, turn by the angle t = pos * rates[i]:
  *   (x, y) -> (x cos t - y sin t, x sin t + y cos t)
- * The angle is formed and reduced to a quarter turn in 64 bits (the product is exact
- * below 2^53), however far the position.  Values and the elements from r on are not
- * rotated.
+ * The angle is formed and reduced to a quarter turn in 64 bits, and with what the
+ * product of position and rate loses past them, however far the position.  Values
+ * and the elements from r on are not rotated.
  */
 typedef struct {
   uint32_t struct_size; /* must be sizeof(tod_append) */

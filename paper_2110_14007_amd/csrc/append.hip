@@ -6,8 +6,9 @@
 // head are a pair (x, y) that turns by the angle pos * rate_i:
 //   x' = x cos - y sin,  y' = x sin + y cos.
 // The angle of a far position has to be right to a small part of a turn, so
-// that it is formed and reduced in 64 bits, where the product of a 32-bit
-// position and a 24-bit rate is exact below 2^53.
+// that it is formed and reduced in 64 bits.  The product of a 32-bit position
+// and a 24-bit rate has up to 55 of them: what it loses past the 53rd is kept
+// beside it.
 //
 // 4-bit rows.  Of 32 elements with the largest magnitude a, the scale 2^e is
 // the smallest with a <= 7 2^e: then the largest error is 2^e, at 7 and
@@ -227,21 +228,25 @@ __device__ __forceinline__ uint32_t encode16(const u32x4& w, uint32_t* scale) {
   return two_codes<ET, 3>(codes, w[3], by);
 }
 
-// Cosine and sine of an angle of fewer than 2^31 radians: the angle less the nearest multiple n of a
-// quarter turn, in two parts (the first difference is exact, for its terms are multiples of 2^-52 and
-// it is small), then the Taylor series to the terms that a T holds, and the quarter's exchange.
+// Cosine and sine of pos * rate: the angle (of fewer than 2^31 radians) less the nearest multiple n of a
+// quarter turn, in two parts (the first difference is exact, for its terms are multiples of 2^-53 and
+// it is small), and what the product lost; then the Taylor series to the terms that a T holds, and the
+// quarter's exchange.
 template <typename T>
-__device__ __forceinline__ void turn_by(double angle, T* cosine, T* sine) {
+__device__ __forceinline__ void turn_by(int32_t pos, float rate, T* cosine, T* sine) {
   constexpr double kQuarter = 0x1.921fb54442d18p+0, kRest = 0x1.1a62633145c07p-54;  // pi / 2
+  const double angle = (double)pos * (double)rate;
+  const double lost = fma((double)pos, (double)rate, -angle);
   if (fabs(angle) >= 0x1p31) {  // (a NaN too, below)
-    double s, c;
+    double s, c, s1, c1;
     sincos(angle, &s, &c);
-    *cosine = (T)c;
-    *sine = (T)s;
+    sincos(lost, &s1, &c1);
+    *cosine = (T)(c * c1 - s * s1);
+    *sine = (T)(s * c1 + c * s1);
     return;
   }
   const double n = rint(angle * 0.63661977236758134308);
-  const T r = (T)fma(-n, kRest, fma(-n, kQuarter, angle));
+  const T r = (T)(fma(-n, kRest, fma(-n, kQuarter, angle)) + lost);
   const T x = r * r;
   T s, c;
   if constexpr (sizeof(T) == 8) {
@@ -302,16 +307,17 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     __syncthreads();  // the tokens before are done with the angles
     for (int i = tid; i < count * half; i += kThreads) {
       const int32_t k = (int32_t)div_by((uint32_t)i, a.angles), m = i - k * half;
-      const double angle = (double)a.pos[t0 + k] * (double)a.rates[m];
+      const int32_t pos = a.pos[t0 + k];
+      const float rate = a.rates[m];
       const int at = place_of<PAIRS>(m, half);
       if constexpr (FOUR) {
         double x, y;
-        turn_by<double>(angle, &x, &y);
+        turn_by<double>(pos, rate, &x, &y);
         turn[k][at] = {(float)x, (float)y};
         turn4[k][at] = {0.5 * x, 0.5 * y};
       } else {
         float x, y;
-        turn_by<float>(angle, &x, &y);
+        turn_by<float>(pos, rate, &x, &y);
         turn[k][at] = {x, y};
       }
     }

@@ -6,7 +6,14 @@ a border and t some parts of a step of b's 32-bit numbers, the element lies that
 the side that t's sign or z's says.  Codes and scales are compared for equality with those of the formula
 in 64 bits, whose rotation is right to 2^-51 of the elements; each case says first that none of its
 elements lies nearer to its border than 2^-32 of it, and that all are within one step of it.
+
+The rotation's angle pos * rate may have 55 bits, two more than 64-bit numbers hold.  The cases of far
+positions look for pairs that the rounded product puts on the wrong side of a border, at least 2^-38
+from it; the angle's sine and cosine come from the product and what it lost, taken exactly.
 """
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
@@ -91,6 +98,54 @@ def test_rotated_next_to_borders(env, layout, name, shift):
         off = abs(y[i, which] * 2.0 ** -shift - b)
         assert 2.0 ** -32 * abs(b) < off < step
     compare(appended(torch, tod, x, pos, rates, layout, name), y, name, lo, hi)
+
+
+def turned(pos, rate):
+    """Cosine and sine of pos * rate with the product's rounding and without it."""
+    exact = Fraction(int(pos)) * Fraction(float(rate))
+    a = float(exact)
+    rest = float(exact - Fraction(a))
+    c, s = math.cos(a), math.sin(a)
+    return (c, s), (c * math.cos(rest) - s * math.sin(rest), s * math.cos(rest) + c * math.sin(rest))
+
+
+@pytest.mark.parametrize("name", ["fp16", "bf16"])
+@pytest.mark.parametrize("layout", sorted(LAYOUTS))
+@pytest.mark.parametrize("least,most", [(0.3, 1.0), (1.0, 7.0)])  # 2^31 radians are passed
+def test_far_positions(env, layout, name, least, most):
+    torch, tod = env
+    dim, r, _ = LAYOUTS[layout]
+    rng = np.random.default_rng(29)
+    bits = 11 if name == "fp16" else 8
+    grid = np.concatenate([2.0 ** e * (1 + np.arange(2 ** (bits - 1)) / 2 ** (bits - 1))
+                           for e in range(-6, 3)])
+    rates = np.zeros(r // 2, np.float32)
+    x, pos, y = [], [], []
+    for pair in range(1, 15):
+        lo, hi = places(layout, pair)
+        rates[pair] = rng.uniform(least, most)
+        for _ in range(16):
+            p = int(rng.integers(2 ** 31 - 2 ** 28, 2 ** 31))
+            (c0, s0), (c, s) = turned(p, rates[pair])
+            for b in BORDERS[:-1]:
+                # For each first element of a pair the second one that comes next to the border.
+                z = (grid * c - b) / s
+                at = np.searchsorted(grid, np.abs(z)).clip(1, len(grid) - 1)
+                at -= np.abs(z) - grid[at - 1] < grid[at] - np.abs(z)
+                z = np.copysign(grid[at], z)
+                off, wrong = grid * c - z * s - b, grid * c0 - z * s0 - b
+                for i in np.nonzero(((off > 0) != (wrong > 0)) & (np.abs(off) > 2.0 ** -38))[0][:4]:
+                    row = np.zeros(dim)
+                    row[places(layout, 0)[0]] = row[places(layout, 0)[1]] = 6.0
+                    row[lo], row[hi] = grid[i], z[i]
+                    x.append(row)
+                    pos.append(p)
+                    y.append(row.copy())
+                    y[-1][lo] = row[lo] * c - row[hi] * s
+                    y[-1][hi] = row[lo] * s + row[hi] * c
+    assert len(x) >= 8
+    got = appended(torch, tod, np.array(x), np.array(pos), rates, layout, name)
+    compare(got, np.array(y), name, 0, 0)
 
 
 @pytest.mark.parametrize("name", ["fp16", "bf16"])
