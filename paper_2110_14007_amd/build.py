@@ -25,7 +25,10 @@ SOURCES = ["api.hip", "prep.hip", "select.hip", "lof.hip", "tile_f32.hip", "tile
 NO_NAN_SOURCES = {"mtile_f16.hip", "mtile_bf16.hip", "tile_f32.hip", "tile_f16.hip",
                   "tile_bf16.hip",
                   # (attention: scores may be NaN.  The maximum leaves them out, exp2 and the
-                  # sums carry them to the output; nothing compares them with themselves.)
+                  # sums carry them to the output; nothing compares them with themselves.
+                  # attn_token4.h holds under either rule: it is compiled under this one as a
+                  # part of attn_tile4_*.hip, and without it in attn_token4_*.hip, whose kernels
+                  # take as many registers with it.)
                   "attn_tile_f16.hip", "attn_tile_bf16.hip", "attn_tile4_f16.hip",
                   "attn_tile4_bf16.hip", "attn_token_f16.hip", "attn_token_bf16.hip"}
 # The attention kernels keep their accumulators in VGPRs (the softmax works on them between two

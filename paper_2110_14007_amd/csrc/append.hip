@@ -20,7 +20,7 @@
 //
 // All three are bound by their bytes, or by their start where there are few.
 // Measured: 48 tokens of 32 + 8 heads of 128 4.8 us; 20,011 of them into 16-bit
-// pages 95 us (492 MB, 5.2 TB/s), 16,001 into a 4-bit cache 79 us (345 MB, 4.4 TB/s:
+// pages 95 us (492 MB, 5.2 TB/s), 16,001 into a 4-bit cache 72 us (345 MB, 4.8 TB/s:
 // the 64-bit rotation of keys takes the rest), 90,001 rows of 8 heads read back
 // 106 us (369 MB written, 98 read, in halves of 128-byte lines: 171 fetched).
 #include "seq.h"

@@ -341,7 +341,7 @@ struct Sum {
   }
 };
 
-// Whether v is neither an infinity nor a NaN.  (These files are compiled as if none met a NaN: the
+// Whether v is neither an infinity nor a NaN.  (These files may be compiled as if none met a NaN: the
 // compiler must not know that the bits are a float's, or it leaves the NaN out of the test.)
 __device__ __forceinline__ bool finite(float v) {
   uint32_t u = __float_as_uint(v);

@@ -5,7 +5,7 @@
 // LDS between the products, word by word: conversions and LDS writes then fill
 // slots that the matrix pipe leaves.  Bound by the products and what is issued
 // beside them, as over 16-bit pages: fewer vector instructions or other orders changed
-// the time by 1% at most, and cards differ by 10 by their clocks.
+// the time by 1% at most, and cards differ by 10% by their clocks.
 //
 // The tiles of all sequences and key / value heads form one line, each as long
 // as the keys that it sees and a constant for its start and its stores, and as
@@ -863,6 +863,8 @@ hipError_t launch_tile4(const AttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// (Rows of 160 to 224 take the products and stages of 256, and their scales and codes a block a lane: a
+// chunk of 512 after 20,000, 16 / 2 heads, rows of 128 120 us, of 192 250, of 256 233.)
 template <typename ET>
 hipError_t launch_tile4(const AttnArgs& a, hipStream_t s) {
   if (a.dim < 64) return launch_tile4<ET, 64, 64, false>(a, s);

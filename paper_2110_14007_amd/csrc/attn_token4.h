@@ -31,7 +31,9 @@
 // us for one of 60,000.  Two waves a SIMD with stages of 64 keys: 171 and 127 us.
 // Pages of 8 rows, whose addresses each lane finds for itself: 97 us for 96 caches
 // of 100 to 8,000, pages of 16 or 64 91.  32 packed rows instead of 4 (a group of 8
-// and 4 new tokens each) over the same caches: 157.
+// and 4 new tokens each) over the same caches: 157, where the bytes alone would take
+// 85: two blocks of rows leave two waves a SIMD, and the second product takes both
+// halves of the weights for each (16 packed rows: 115).
 #pragma once
 
 #include "attn_token.h"
