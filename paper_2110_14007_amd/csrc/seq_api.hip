@@ -188,7 +188,10 @@ tod_status run_attn(const tod_attn& o, tod::AttnArgs* a, const Plan& p, Form for
   if (!p.fits) return unsupported("too many rows for one call");
   if (!aligned(ws, 256)) return set_error(TOD_ERR_WORKSPACE, "workspace misaligned");
   if (ws_bytes < p.total)
-    return set_error(TOD_ERR_WORKSPACE, "workspace smaller than tod_attn_workspace_size()");
+    return set_error(TOD_ERR_WORKSPACE,
+                     form == Form::kPaged4
+                         ? "workspace smaller than tod_attn_paged4_workspace_size()"
+                         : "workspace smaller than tod_attn_workspace_size()");
   char* const base = (char*)ws;
   a->skip_rows = p.skip_rows;
   a->token_tail = p.tile ? 0 : 1;
